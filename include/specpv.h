@@ -352,6 +352,81 @@ specpv_status specpv_verify_full_offloaded(const specpv_config *cfg, int layer0,
                                            void *out, float *lse, void *workspace, size_t workspace_bytes,
                                            void *stream, void *copy_stream);
 
+/* ---- Full KV cache in 4 bits -----------------------------------------------------------------------
+ * (No counterpart in the paper.)  A full cache that takes d + 8 bytes per token and KV head instead of 4 d: 136 against 512
+ * at 128 channels of bfloat16.  Every row (a token's key or value of one KV head) is quantised by itself:
+ *   scale = bfloat16((max - min) / 15),  offset = bfloat16(min - 16 scale),  code n = the nearest of 0 .. 15 (ties to even)
+ * and code n stands for bfloat16((16 + n) * scale + offset), rounded once.  A row that holds an infinity or a NaN, or whose range
+ * bfloat16 cannot hold, is stored as NaN.  Attention, summaries and the partial cache taken out of it all see these bfloat16 values.
+ *
+ *   pool   [n_layers][n_pages][Hkv][bs (d + 8) bytes], a page of a KV head being
+ *          key codes [d / 32][bs][16 bytes] | value codes [bs / 16][d][8 bytes] | [4][bs] bfloat16: key scales, key offsets, value
+ *          scales, value offsets.  A 32-bit word holds eight codes, of consecutive channels (keys) or tokens (values): element 2 i in
+ *          bits 4 i .. 4 i + 3, element 2 i + 1 in bits 16 + 4 i .. 19 + 4 i, the word then rotated left by three bits.
+ * The step's own tensors (q, k_new, v_new, out) are of cfg->dtype, as everywhere. */
+typedef struct {
+    void *pool;                 /* device */
+    const int32_t *block_table; /* device, [batch][max_blocks] */
+    const int32_t *seq_lens;    /* device, [batch] */
+    int32_t batch;
+    int32_t max_blocks;
+    int32_t n_pages;
+    int32_t max_seq_len; /* host-known upper bound of seq_lens[], used only to size grids */
+} specpv_paged_q4;
+
+/* specpv_verify_full over a cache in 4 bits: the same arguments, masks, outputs and workspace; M_max = 1 is plain decoding.
+ * A row that sees nothing (an empty cache and an empty row of the mask) gets out = 0 and lse = -infinity.  Infinities and NaN in
+ * k_new and v_new reach the rows that see their token and no others. */
+specpv_status specpv_verify_full_q4(const specpv_config *cfg, int layer0, int n_layers, const void *q, const void *k_new,
+                                    const void *v_new, const uint64_t *tree_mask, const int32_t *q_lens, int M_max,
+                                    const specpv_paged_q4 *full, void *out, float *lse, void *workspace,
+                                    size_t workspace_bytes, void *stream);
+
+/* specpv_commit_accepted into a cache in 4 bits: the rows are quantised as they are appended.  accepted may be NULL: rows
+ * 0 .. n_accepted[b] - 1 in order, A_max <= M_max, which here may be any number (a chunk of a prefill).  kmax / kmin (both or
+ * neither): the summaries of the blocks that received tokens, over the values that their keys stand for.  k_values / v_values (both
+ * or neither; [n_layers_in_call][batch][A_max][Hkv][d] of cfg->dtype): what the appended rows stand for, so that a caller can append
+ * the same numbers to another cache; rows >= n_accepted[b] are left as they were.  A row number outside [0, M_max) is
+ * recorded as SPECPV_ERR_INVALID_ARG and its token left as its place was.  Pages that receive tokens belong to one sequence. */
+specpv_status specpv_commit_accepted_q4(const specpv_config *cfg, int layer0, int n_layers, const void *k_new,
+                                        const void *v_new, int M_max, const int32_t *accepted, const int32_t *n_accepted,
+                                        int A_max, const specpv_paged_q4 *dst, void *kmax, void *kmin, void *k_values,
+                                        void *v_values, void *workspace, size_t workspace_bytes, void *stream);
+
+/* specpv_refresh_partial out of a cache in 4 bits: the selected blocks are opened into the partial cache (of cfg->dtype). */
+specpv_status specpv_refresh_partial_q4(const specpv_config *cfg, const specpv_paged_q4 *full, const int32_t *idx,
+                                        const int32_t *count, const specpv_paged_kv *partial, int32_t *partial_lens,
+                                        void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- Eviction by accumulated attention weight --------------------------------------------------------
+ * (No counterpart in the paper: the other way to bound a cache, token by token and for good.)  acc, [n_layers][batch][Hkv]
+ * [max_blocks * bs] float32, holds the attention weight that every token of a cache has received so far, summed over the query
+ * heads of its KV head; the caller zeroes it once. */
+
+/* After a step's accepted rows have been committed to kv (an ordinary cache, full or partial):
+ *   acc[t] += sum over i < n_accepted[b] and heads of exp(scale q_i . k_t - lse_i)   for t < seq_lens[b] - n_accepted[b] + i + 1
+ * where row i is row accepted[b][i] (accepted = NULL: row i, A_max <= M_max) of q and lse, lse being what the verify call wrote: row i
+ * sees the cache up to its own token, its ancestors being the rows before it.  A chunk of a prefill or a decoded token is the
+ * same with accepted = NULL.  q and lse are indexed by layer-in-call, acc by model layer.  A row whose lse is -infinity adds
+ * nothing; a row number outside [0, M_max) is recorded as SPECPV_ERR_INVALID_ARG and skipped.  The sums do not depend on the
+ * order in which the GPU runs them.  M_max is at most 128. */
+specpv_status specpv_accumulate_attention(const specpv_config *cfg, int layer0, int n_layers, const void *q, const float *lse,
+                                          int M_max, const int32_t *accepted, const int32_t *n_accepted, int A_max,
+                                          const specpv_paged_kv *kv, float *acc, void *workspace, size_t workspace_bytes,
+                                          void *stream);
+
+/* Every sequence that holds more than keep_tokens tokens is cut down to keep_tokens: the first sink_tokens, the last
+ * local_tokens, and of the others those with the most accumulated weight (ties to the lower token, NaN last; with
+ * cfg->select_shared ranked on the mean over the KV heads), separately for every layer and KV head.  They close up in place, in
+ * order, in all layers of kv; acc moves with them, the accounts of the places that became free are set to zero, and
+ * seq_lens[b] = keep_tokens.  Rows behind the new end keep what they held; shorter sequences are not touched.  idx (device,
+ * [n_layers][batch][Hkv][keep_tokens]) receives the token that each place now holds (the first min(seq_lens[b], keep_tokens)).
+ * keep_tokens < sink_tokens + local_tokens + 1 is SPECPV_ERR_BUDGET.  Pages must not be shared between sequences.  Block
+ * summaries are not updated: specpv_update_block_summaries does that. */
+specpv_status specpv_evict_tokens(const specpv_config *cfg, const specpv_paged_kv *kv, float *acc, int keep_tokens,
+                                  int sink_tokens, int local_tokens, int32_t *idx, void *workspace, size_t workspace_bytes,
+                                  void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,6 +33,7 @@ EXPORTS = [
     "specpv_select_partial_kv", "specpv_refresh_partial", "specpv_verify_partial",
     "specpv_verify_full", "specpv_verify_host", "specpv_commit_accepted", "specpv_verify_partial_static",
     "specpv_rope_table", "specpv_qkv_rope", "specpv_o_proj", "specpv_verify_full_offloaded",
+    "specpv_verify_full_q4", "specpv_commit_accepted_q4", "specpv_refresh_partial_q4", "specpv_accumulate_attention", "specpv_evict_tokens",
 ]
 
 
@@ -63,20 +64,22 @@ class PagedKV(ctypes.Structure):
                 ("n_pages", c_int32), ("max_seq_len", c_int32)]
 
 
-# The calls of a step by the kinds of their Python arguments, as in pycalls.c: G Config, i int, P tensor or None, C Cache,
+# The calls of a step by the kinds of their Python arguments, as in pycalls.c: G Config, i int, P tensor or None, C Cache, Q CacheQ4,
 # W workspace tensor (pointer and bytes), S stream.
 _STEP_CALLS = {
     "specpv_update_block_summaries": "GiiCPiPPWS", "specpv_score_blocks": "GiiPPiPPPCPWS", "specpv_select_partial_kv": "GiPPiiPPWS",
     "specpv_refresh_partial": "GCPPCPWS", "specpv_verify_partial": "GiiPPPPPiCPPWS", "specpv_verify_full": "GiiPPPPPiCPPWS",
     "specpv_verify_partial_static": "GiiPPPPPiCPPPS", "specpv_verify_host": "GiiiPPPPiCPPWS",
     "specpv_commit_accepted": "GiiPPiPPiCPPWS", "specpv_qkv_rope": "GiiPiPPiiPPPWS", "specpv_o_proj": "GiiPPiPiiPWS",
+    "specpv_verify_full_q4": "GiiPPPPPiQPPWS", "specpv_commit_accepted_q4": "GiiPPiPPiQPPPPWS", "specpv_refresh_partial_q4": "GQPPCPWS",
+    "specpv_accumulate_attention": "GiiPPiPPiCPWS", "specpv_evict_tokens": "GCPiiiPWS",
 }
 # C argument kinds (P pointer, i int32, z size_t, d double): declared, so that plain Python numbers can be passed.
 # A call of the step is a few microseconds of device work, and wrapping every argument in a ctypes object cost as much.
 _SIGNATURES = {
     "specpv_poll_status": "PPP", "specpv_build_tree_mask": "PiiPi", "specpv_select_mode": "iiiiii", "specpv_rope_table": "PPPPiidPP",
     "specpv_verify_full_offloaded": "PiiPPPPPiPPPPzPP", "specpv_selftest_wait_timeout": "PziPP",
-    **{name: kinds.translate(str.maketrans({"G": "P", "C": "P", "W": "Pz", "S": "P"})) for name, kinds in _STEP_CALLS.items()},
+    **{name: kinds.translate(str.maketrans({"G": "P", "C": "P", "Q": "P", "W": "Pz", "S": "P"})) for name, kinds in _STEP_CALLS.items()},
 }
 _KINDS = {"P": c_void_p, "i": c_int, "z": c_size_t, "d": c_double}
 
@@ -127,7 +130,7 @@ class _CtypesCalls:
             for kind, arg in zip(kinds, args, strict=True):
                 if kind == "G":
                     values.append(byref(arg))
-                elif kind == "C":
+                elif kind in "CQ":
                     values.append(byref(arg.desc()))
                 elif kind == "S":
                     values.append(_stream(arg))
@@ -371,3 +374,58 @@ def specpv_verify_full_offloaded(cfg, layer0, n_layers, q, k_new, v_new, tree_ma
                                               _ptr(lse), _ptr(workspace), workspace.numel(),
                                               _stream(stream), _stream(copy_stream)),
            "specpv_verify_full_offloaded")
+
+
+# ---- full KV cache in 4 bits ------------------------------------------------------------------------------------
+class PagedQ4(ctypes.Structure):
+    """Mirror of ``specpv_paged_q4``."""
+    _fields_ = [("pool", c_void_p), ("block_table", c_void_p), ("seq_lens", c_void_p), ("batch", c_int32), ("max_blocks", c_int32),
+                ("n_pages", c_int32), ("max_seq_len", c_int32)]
+
+
+@dataclass
+class CacheQ4:
+    """A paged KV cache in 4 bits: one pool of bytes for keys, values and their scales (``new_q4_pool``)."""
+    pool: torch.Tensor         # [n_layers][n_pages][Hkv][bs (d + 8)] uint8
+    block_table: torch.Tensor  # [batch][max_blocks] int32
+    seq_lens: torch.Tensor     # [batch] int32
+    max_seq_len: int
+
+    def desc(self) -> PagedQ4:
+        pool, table = self.pool, self.block_table
+        return PagedQ4(pool.data_ptr(), table.data_ptr(), self.seq_lens.data_ptr(), table.size(0), table.size(1), pool.size(1),
+                       int(self.max_seq_len))
+
+
+def new_q4_pool(cfg: Config, n_pages: int, device="cuda") -> torch.Tensor:
+    """A zeroed pool for ``n_pages`` pages of a cache in 4 bits."""
+    return torch.zeros(cfg.n_layers, n_pages, cfg.n_kv_heads, cfg.block_tokens * (cfg.head_dim + 8), dtype=torch.uint8, device=device)
+
+
+def specpv_verify_full_q4(cfg, layer0, n_layers, q, k_new, v_new, tree_mask, q_lens, M_max, full: CacheQ4, out, lse, workspace,
+                          stream=None):
+    _verify("specpv_verify_full_q4", cfg, layer0, n_layers, q, k_new, v_new, tree_mask, q_lens, M_max, full, out, lse, workspace,
+            stream)
+
+
+def specpv_commit_accepted_q4(cfg, layer0, n_layers, k_new, v_new, M_max, accepted, n_accepted, A_max, dst: CacheQ4, kmax, kmin,
+                              k_values, v_values, workspace, stream=None):
+    _check(_native().specpv_commit_accepted_q4(cfg, layer0, n_layers, k_new, v_new, M_max, accepted, n_accepted, A_max, dst, kmax,
+                                               kmin, k_values, v_values, workspace, stream), "specpv_commit_accepted_q4")
+
+
+def specpv_refresh_partial_q4(cfg, full: CacheQ4, idx, count, partial: Cache, partial_lens, workspace, stream=None):
+    _check(_native().specpv_refresh_partial_q4(cfg, full, idx, count, partial, partial_lens, workspace, stream),
+           "specpv_refresh_partial_q4")
+
+
+# ---- eviction by accumulated attention weight -------------------------------------------------------------------
+def specpv_accumulate_attention(cfg, layer0, n_layers, q, lse, M_max, accepted, n_accepted, A_max, kv: Cache, acc, workspace,
+                                stream=None):
+    _check(_native().specpv_accumulate_attention(cfg, layer0, n_layers, q, lse, M_max, accepted, n_accepted, A_max, kv, acc,
+                                                 workspace, stream), "specpv_accumulate_attention")
+
+
+def specpv_evict_tokens(cfg, kv: Cache, acc, keep_tokens, sink_tokens, local_tokens, idx, workspace, stream=None):
+    _check(_native().specpv_evict_tokens(cfg, kv, acc, keep_tokens, sink_tokens, local_tokens, idx, workspace, stream),
+           "specpv_evict_tokens")

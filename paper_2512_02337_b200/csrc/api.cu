@@ -7,6 +7,7 @@
 #include "aux_kernels.cuh"
 #include "common.cuh"
 #include "proj.cuh"
+#include "q4.cuh"
 
 #define SPECPV_EXPORT extern "C" __attribute__((visibility("default")))
 
@@ -57,6 +58,14 @@ specpv_status validate_kv(const Geometry& g, const specpv_paged_kv* kv) {
     (void)g;
     if (!kv || !kv->k_pool || !kv->v_pool || !kv->block_table || !kv->seq_lens) return SPECPV_ERR_INVALID_ARG;
     if (!aligned16(kv->k_pool) || !aligned16(kv->v_pool)) return SPECPV_ERR_INVALID_ARG;
+    if (kv->batch <= 0 || kv->max_blocks <= 0 || kv->n_pages <= 0 || kv->max_seq_len < 0) return SPECPV_ERR_INVALID_ARG;
+    if ((int64_t)kv->max_seq_len > (int64_t)kv->max_blocks * g.bs) return SPECPV_ERR_CAPACITY;
+    return SPECPV_OK;
+}
+
+static specpv_status validate_q4(const Geometry& g, const specpv_paged_q4* kv) {
+    if (!kv || !kv->pool || !kv->block_table || !kv->seq_lens) return SPECPV_ERR_INVALID_ARG;
+    if (!aligned16(kv->pool)) return SPECPV_ERR_INVALID_ARG;
     if (kv->batch <= 0 || kv->max_blocks <= 0 || kv->n_pages <= 0 || kv->max_seq_len < 0) return SPECPV_ERR_INVALID_ARG;
     if ((int64_t)kv->max_seq_len > (int64_t)kv->max_blocks * g.bs) return SPECPV_ERR_CAPACITY;
     return SPECPV_OK;
@@ -598,4 +607,129 @@ SPECPV_EXPORT specpv_status specpv_o_proj(const specpv_config* cfg, int layer0, 
     a.n_seg = 1;
     a.seg[0] = ProjSegment{y, 0, hidden, 0};
     return proj_dispatch(a, g, layer0, n_layers, batch, M_max, workspace, workspace_bytes, stream);
+}
+
+// ---- a cache in 4 bits ------------------------------------------------------------------------------------------
+SPECPV_EXPORT specpv_status specpv_verify_full_q4(const specpv_config* cfg, int layer0, int n_layers, const void* q, const void* k_new,
+                                                  const void* v_new, const uint64_t* tree_mask, const int32_t* q_lens, int M_max,
+                                                  const specpv_paged_q4* full, void* out, float* lse, void* workspace,
+                                                  size_t workspace_bytes, void* stream) {
+    Geometry g;
+    specpv_status st = validate_config(cfg, &g);
+    if (st != SPECPV_OK) return st;
+    st = validate_q4(g, full);
+    if (st != SPECPV_OK) return st;
+    if (!q || !k_new || !v_new || !tree_mask || !out || !workspace) return SPECPV_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out) || !aligned16(workspace)) return SPECPV_ERR_INVALID_ARG;
+    if (layer0 < 0 || n_layers <= 0 || layer0 + n_layers > g.n_layers || M_max <= 0) return SPECPV_ERR_INVALID_ARG;
+    if (M_max > kMaxQTokens) return SPECPV_ERR_CAPACITY;
+    const WorkspacePlan w = plan_workspace(g, n_layers, full->batch, M_max);
+    if (workspace_bytes < w.partial_off + w.partial_bytes) return SPECPV_ERR_CAPACITY;
+    AttnArgs a{};
+    a.g = g;
+    a.layer0 = layer0; a.n_layers = n_layers; a.batch = full->batch; a.M_max = M_max;
+    a.mask_words = (M_max + 63) / 64;
+    a.q = q; a.k_new = k_new; a.v_new = v_new; a.tree_mask = tree_mask; a.q_lens = q_lens;
+    a.q4_pool = full->pool; a.block_table = full->block_table; a.seq_lens = full->seq_lens;
+    a.max_blocks = full->max_blocks; a.n_pages = full->n_pages; a.max_seq_len = full->max_seq_len;
+    a.out = out; a.lse = lse; a.workspace = workspace;
+    a.partial_off = w.partial_off;
+    a.partial_bytes = w.partial_bytes;
+    return launch_attention_simt(a, reinterpret_cast<cudaStream_t>(stream));
+}
+
+SPECPV_EXPORT specpv_status specpv_commit_accepted_q4(const specpv_config* cfg, int layer0, int n_layers, const void* k_new,
+                                                      const void* v_new, int M_max, const int32_t* accepted,
+                                                      const int32_t* n_accepted, int A_max, const specpv_paged_q4* dst, void* kmax,
+                                                      void* kmin, void* k_values, void* v_values, void* workspace,
+                                                      size_t workspace_bytes, void* stream) {
+    Geometry g;
+    specpv_status st = validate_config(cfg, &g);
+    if (st != SPECPV_OK) return st;
+    st = validate_q4(g, dst);
+    if (st != SPECPV_OK) return st;
+    if (!k_new || !v_new || !n_accepted || !workspace || workspace_bytes < kStatusBytes) return SPECPV_ERR_INVALID_ARG;
+    if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_values) || !aligned16(v_values)) return SPECPV_ERR_INVALID_ARG;
+    if ((kmax == nullptr) != (kmin == nullptr) || (k_values == nullptr) != (v_values == nullptr)) return SPECPV_ERR_INVALID_ARG;
+    if (layer0 < 0 || n_layers <= 0 || layer0 + n_layers > g.n_layers || M_max <= 0 || A_max <= 0) return SPECPV_ERR_INVALID_ARG;
+    if (!accepted && A_max > M_max) return SPECPV_ERR_CAPACITY;
+    CommitQ4Params p{};
+    p.k_new = k_new; p.v_new = v_new; p.accepted = accepted; p.n_accepted = n_accepted; p.pool = dst->pool;
+    p.block_table = dst->block_table; p.seq_lens = const_cast<int32_t*>(dst->seq_lens); p.kmax = kmax; p.kmin = kmin;
+    p.k_values = k_values; p.v_values = v_values; p.workspace = workspace;
+    p.layer0 = layer0; p.batch = dst->batch; p.M_max = M_max; p.A_max = A_max; p.Hkv = g.Hkv; p.bs = g.bs;
+    p.max_blocks = dst->max_blocks; p.n_pages = dst->n_pages;
+    return launch_commit_q4(p, n_layers, g.dtype, g.d, layer0 + n_layers == g.n_layers, reinterpret_cast<cudaStream_t>(stream));
+}
+
+SPECPV_EXPORT specpv_status specpv_refresh_partial_q4(const specpv_config* cfg, const specpv_paged_q4* full, const int32_t* idx,
+                                                      const int32_t* count, const specpv_paged_kv* partial, int32_t* partial_lens,
+                                                      void* workspace, size_t workspace_bytes, void* stream) {
+    Geometry g;
+    specpv_status st = validate_config(cfg, &g);
+    if (st != SPECPV_OK) return st;
+    st = validate_q4(g, full);
+    if (st != SPECPV_OK) return st;
+    if (!partial || !partial->k_pool || !partial->v_pool || !partial->block_table) return SPECPV_ERR_INVALID_ARG;
+    if (!aligned16(partial->k_pool) || !aligned16(partial->v_pool)) return SPECPV_ERR_INVALID_ARG;
+    if (!idx || !count || !partial_lens || !workspace || workspace_bytes < kStatusBytes) return SPECPV_ERR_INVALID_ARG;
+    if (partial->batch != full->batch || partial->n_pages <= 0) return SPECPV_ERR_INVALID_ARG;
+    if ((int64_t)partial->max_blocks * g.bs < (int64_t)g.budget_blocks * g.bs + g.buffer_tokens) return SPECPV_ERR_CAPACITY;
+    GatherQ4Params p{};
+    p.pool = full->pool; p.full_table = full->block_table; p.seq_lens = full->seq_lens; p.idx = idx; p.count = count;
+    p.part_k = partial->k_pool; p.part_v = partial->v_pool; p.part_table = partial->block_table; p.partial_lens = partial_lens;
+    p.workspace = workspace;
+    p.batch = full->batch; p.Hkv = g.Hkv; p.bs = g.bs; p.budget_blocks = g.budget_blocks; p.full_max_blocks = full->max_blocks;
+    p.full_pages = full->n_pages; p.part_max_blocks = partial->max_blocks; p.part_pages = partial->n_pages;
+    return launch_gather_q4(p, g.n_layers, g.dtype, g.d, reinterpret_cast<cudaStream_t>(stream));
+}
+
+// ---- eviction by accumulated attention weight -------------------------------------------------------------------
+SPECPV_EXPORT specpv_status specpv_accumulate_attention(const specpv_config* cfg, int layer0, int n_layers, const void* q,
+                                                        const float* lse, int M_max, const int32_t* accepted,
+                                                        const int32_t* n_accepted, int A_max, const specpv_paged_kv* kv, float* acc,
+                                                        void* workspace, size_t workspace_bytes, void* stream) {
+    Geometry g;
+    specpv_status st = validate_config(cfg, &g);
+    if (st != SPECPV_OK) return st;
+    st = validate_kv(g, kv);
+    if (st != SPECPV_OK) return st;
+    if (!q || !lse || !n_accepted || !acc || !workspace || workspace_bytes < kStatusBytes) return SPECPV_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(acc)) return SPECPV_ERR_INVALID_ARG;
+    if (layer0 < 0 || n_layers <= 0 || layer0 + n_layers > g.n_layers || M_max <= 0 || A_max <= 0) return SPECPV_ERR_INVALID_ARG;
+    if (M_max > kMaxQTokens || (!accepted && A_max > M_max)) return SPECPV_ERR_CAPACITY;
+    AccumulateParams p{};
+    p.q = q; p.lse = lse; p.accepted = accepted; p.n_accepted = n_accepted; p.k_pool = kv->k_pool; p.block_table = kv->block_table;
+    p.seq_lens = kv->seq_lens; p.acc = acc; p.workspace = workspace;
+    p.layer0 = layer0; p.batch = kv->batch; p.M_max = M_max; p.A_max = A_max; p.Hq = g.Hq; p.Hkv = g.Hkv; p.G = g.G; p.bs = g.bs;
+    p.max_blocks = kv->max_blocks; p.n_pages = kv->n_pages; p.scale = g.scale;
+    return launch_accumulate(p, n_layers, kv->max_seq_len, g.dtype, g.d, reinterpret_cast<cudaStream_t>(stream));
+}
+
+SPECPV_EXPORT specpv_status specpv_evict_tokens(const specpv_config* cfg, const specpv_paged_kv* kv, float* acc, int keep_tokens,
+                                                int sink_tokens, int local_tokens, int32_t* idx, void* workspace,
+                                                size_t workspace_bytes, void* stream) {
+    Geometry g;
+    specpv_status st = validate_config(cfg, &g);
+    if (st != SPECPV_OK) return st;
+    st = validate_kv(g, kv);
+    if (st != SPECPV_OK) return st;
+    if (!acc || !idx || !workspace || workspace_bytes < kStatusBytes || !aligned16(acc)) return SPECPV_ERR_INVALID_ARG;
+    if (sink_tokens < 0 || local_tokens < 0 || (int64_t)keep_tokens < (int64_t)sink_tokens + local_tokens + 1) return SPECPV_ERR_BUDGET;
+    if (kv->batch > 65535 || g.n_layers > 65535 || (int64_t)g.n_layers * kv->batch > 65535) return SPECPV_ERR_CAPACITY;
+    if ((int64_t)kv->max_blocks * g.bs > 0x7FFFFFFF) return SPECPV_ERR_CAPACITY;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    // a token is a block of one: the selection of blocks (ties, NaN, select_shared) serves as it is
+    SelectParams c{};
+    c.scores = acc; c.seq_lens = kv->seq_lens; c.idx = idx; c.batch = kv->batch; c.Hkv = g.Hkv; c.bs = 1;
+    c.max_blocks = kv->max_blocks * g.bs; c.sink_blocks = sink_tokens; c.local_blocks = local_tokens; c.budget_blocks = keep_tokens;
+    c.share_heads = g.select_shared;
+    st = launch_select(c, g.n_layers, s);
+    if (st != SPECPV_OK) return st;
+    EvictParams p{};
+    p.k_pool = kv->k_pool; p.v_pool = kv->v_pool; p.block_table = kv->block_table; p.seq_lens = const_cast<int32_t*>(kv->seq_lens);
+    p.acc = acc; p.idx = idx; p.workspace = workspace;
+    p.batch = kv->batch; p.Hkv = g.Hkv; p.bs = g.bs; p.row_bytes = g.d * g.es; p.keep = keep_tokens; p.max_blocks = kv->max_blocks;
+    p.n_pages = kv->n_pages;
+    return launch_evict(p, g.n_layers, s);
 }

@@ -16,6 +16,7 @@
 #include <math.h>
 
 #include "common.cuh"
+#include "q4.cuh"
 #include "tc_common.cuh"
 
 namespace specpv {
@@ -41,6 +42,7 @@ struct SimtParams {
     const int32_t* q_lens;
     const void* k_pool;
     const void* v_pool;
+    const void* q4_pool;  // kQ4: a cache in 4 bits instead
     const int32_t* block_table;
     const int32_t* seq_lens;
     void* out;
@@ -73,7 +75,26 @@ __device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
                        __uint_as_float(w.y & 0xFFFF0000u));
 }
 
-template <typename T, typename TO, int D>
+// four channels from c on of token t's key or value in a page of a cache in 4 bits
+__device__ __forceinline__ float4 open_key(const uint32_t* page, int bs, int d, int t, int c) {
+    const uint16_t* params = reinterpret_cast<const uint16_t*>(page);
+    const uint32_t scale = q4::twice(params[q4::param_at(bs, d, 0, t)]), offset = q4::twice(params[q4::param_at(bs, d, 1, t)]);
+    const uint32_t w = page[q4::k_word(bs, t, c)];
+    const uint32_t a = q4::fma_bf16x2(q4::open_pair(w, c & 4 ? 2 : 0), scale, offset), z = q4::fma_bf16x2(q4::open_pair(w, c & 4 ? 3 : 1), scale, offset);
+    return make_float4(q4::lower(a), q4::upper(a), q4::lower(z), q4::upper(z));
+}
+__device__ __forceinline__ float4 open_value(const uint32_t* page, int bs, int d, int t, int c) {
+    const uint16_t* params = reinterpret_cast<const uint16_t*>(page);
+    const uint16_t scale = params[q4::param_at(bs, d, 2, t)], offset = params[q4::param_at(bs, d, 3, t)];
+    const uint32_t* w = page + q4::v_word(bs, d, t, c);
+    return make_float4(q4::value_of(w[0], t & 7, scale, offset), q4::value_of(w[2], t & 7, scale, offset),
+                       q4::value_of(w[4], t & 7, scale, offset), q4::value_of(w[6], t & 7, scale, offset));
+}
+
+// kQ4: the cache is one in 4 bits, whose codes are opened as they are fetched.  Also, a row that sees nothing comes out as zeros, and
+// an infinity or NaN among the step's own values reaches the rows that see its token and no others: such an element takes no part
+// in the products (0 times it would be NaN) and is added to the sums of the rows that see it, whose weight of it is positive.
+template <typename T, typename TO, int D, bool kQ4>
 __global__ void __launch_bounds__(kThreads) attn_simt_kernel(SimtParams p) {
     pdl_begin(p.pdl);
     constexpr int CPT = D / 16;   // output channels per thread
@@ -90,7 +111,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(SimtParams p) {
     const int h = blockIdx.y, lb = blockIdx.z;
     const int b = lb % p.batch, l = lb / p.batch;
     const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
-    const int seq_len = max(p.seq_lens[b], 0);
+    const int seq_len = kQ4 ? (int)min((long long)max(p.seq_lens[b], 0), (long long)p.max_blocks * p.bs) : max(p.seq_lens[b], 0);
     int M = p.q_lens ? p.q_lens[b] : p.M_max;
     M = min(max(M, 0), p.M_max);
     const int R = M * p.G, R_max = p.M_max * p.G;
@@ -134,6 +155,21 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(SimtParams p) {
     bool exists = false;
     auto fetch = [&](int tile) {
         const T *ks = nullptr, *vs = nullptr;
+        if (kQ4 && tile < ctx_tiles) {
+            const int t = tile * kTok + st;
+            const int page = t < seq_len ? table[t / p.bs] : 0;
+            exists = t < seq_len && page >= 0 && page < p.n_pages;
+            if (t < seq_len && !exists && sc == 0 && row0 == 0) record_fault(p.workspace, SPECPV_ERR_BAD_BLOCK_TABLE, b, t / p.bs, page, l);
+            const uint32_t* words = reinterpret_cast<const uint32_t*>(
+                reinterpret_cast<const char*>(p.q4_pool) + (((size_t)(p.layer0 + l) * p.n_pages + (exists ? page : 0)) * p.Hkv + h) * q4::page_bytes(p.bs, D));
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int c = (sc + 4 * i) * 4;
+                kbuf[i] = exists ? open_key(words, p.bs, D, t % p.bs, c) : make_float4(0.f, 0.f, 0.f, 0.f);
+                vbuf[i] = exists ? open_value(words, p.bs, D, t % p.bs, c) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            return;
+        }
         if (tile < ctx_tiles) {
             const int t = tile * kTok + st;
             if (t < seq_len) {
@@ -171,6 +207,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(SimtParams p) {
     for (int tile = tile_begin; tile < tile_end; ++tile) {
         const bool is_new = tile >= ctx_tiles;
         const int tok0 = (is_new ? tile - ctx_tiles : tile) * kTok;
+        int odd = 0;  // kQ4: the tile holds an infinite or NaN value
         __syncthreads();  // the previous tile has been read
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -179,10 +216,20 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(SimtParams p) {
             Kt[(c + 1) * kPitch + st] = kbuf[i].y;
             Kt[(c + 2) * kPitch + st] = kbuf[i].z;
             Kt[(c + 3) * kPitch + st] = kbuf[i].w;
+            if (kQ4 && is_new) {
+                float v[4] = {vbuf[i].x, vbuf[i].y, vbuf[i].z, vbuf[i].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    odd |= !isfinite(v[e]);
+                    v[e] = isfinite(v[e]) ? v[e] : 0.f;
+                }
+                vbuf[i] = make_float4(v[0], v[1], v[2], v[3]);
+            }
             *reinterpret_cast<float4*>(Vs + st * D + c) = vbuf[i];
         }
         if (sc == 0) s_exists[st] = exists;
-        __syncthreads();
+        if (kQ4 && is_new) odd = __syncthreads_or(odd);
+        else __syncthreads();
         if (tile + 1 < tile_end) fetch(tile + 1);
         // S = Q K^T: rows 4 ty .. + 3, tokens 4 tx .. + 3.  Channels are summed in runs of 16, the runs then added: the
         // rounding of a long serial sum would show in the weights of the largest logits.
@@ -275,6 +322,19 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(SimtParams p) {
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int c = 0; c < CPT; ++c) acc[i][c] = fmaf(acc[i][c], corr[i], c % 2 ? tile_acc[i][c / 2].y : tile_acc[i][c / 2].x);
+        if (kQ4 && odd) {
+            for (int t = 0; t < kTok && tok0 + t < M; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (!(s_mask[4 * ty + i][(tok0 + t) >> 6] >> ((tok0 + t) & 63) & 1)) continue;
+                    const T* v = v_new + ((size_t)(tok0 + t) * p.Hkv + h) * D;
+#pragma unroll
+                    for (int c = 0; c < CPT; ++c) {
+                        const float x = to_float<T>(v[c / 4 * 64 + 4 * tx + c % 4]);
+                        if (!isfinite(x)) acc[i][c] += x;
+                    }
+                }
+        }
     }
     // acc[i][c .. c + 3] are channels 16 c + 4 tx .. + 3 of row 4 ty + i
 #pragma unroll
@@ -285,7 +345,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(SimtParams p) {
             const int j = r / p.G, g = r % p.G;
             const size_t row = ((size_t)lb * p.M_max + j) * p.Hq + h * p.G + g;
             TO* o = reinterpret_cast<TO*>(p.out) + row * D;
-            const float inv = 1.f / l_run[i];
+            const float inv = kQ4 && l_run[i] == 0.f ? 0.f : 1.f / l_run[i];
 #pragma unroll
             for (int c = 0; c < CPT; ++c) o[c / 4 * 64 + 4 * tx + c % 4] = from_float<TO>(acc[i][c] * inv);
             if (p.lse && tx == 0) p.lse[row] = m_run[i] + logf(l_run[i]);
@@ -382,7 +442,7 @@ __global__ void __launch_bounds__(kMergeThreads) merge_splits_kernel(SimtParams 
     const int j = r / p.G, g = r % p.G;
     const size_t row = ((size_t)lb * p.M_max + j) * p.Hq + h * p.G + g;
     TO* dst = reinterpret_cast<TO*>(p.out) + row * D + lane * 4;
-    const float inv = 1.f / l_all;
+    const float inv = p.q4_pool && l_all == 0.f ? 0.f : 1.f / l_all;
     dst[0] = from_float<TO>(o.x * inv);
     dst[1] = from_float<TO>(o.y * inv);
     dst[2] = from_float<TO>(o.z * inv);
@@ -390,12 +450,12 @@ __global__ void __launch_bounds__(kMergeThreads) merge_splits_kernel(SimtParams 
     if (p.lse && lane == 0) p.lse[row] = m_all + logf(l_all);
 }
 
-template <typename T, typename TO, int D>
+template <typename T, typename TO, int D, bool kQ4>
 specpv_status launch_typed(const AttnArgs& a, SimtParams& p, cudaStream_t stream) {
     constexpr size_t smem = simt_smem<D>();
-    if (!tc::set_smem_limit_once(reinterpret_cast<const void*>(attn_simt_kernel<T, TO, D>), (int)smem)) return SPECPV_ERR_CUDA;
+    if (!tc::set_smem_limit_once(reinterpret_cast<const void*>(attn_simt_kernel<T, TO, D, kQ4>), (int)smem)) return SPECPV_ERR_CUDA;
     dim3 grid(p.n_splits * p.row_tiles, a.g.Hkv, a.n_layers * a.batch);
-    if (launch_pdl_if(attn_simt_kernel<T, TO, D>, grid, kThreads, smem, stream, p) != cudaSuccess) return SPECPV_ERR_CUDA;
+    if (launch_pdl_if(attn_simt_kernel<T, TO, D, kQ4>, grid, kThreads, smem, stream, p) != cudaSuccess) return SPECPV_ERR_CUDA;
     count_launch();
     if (p.n_splits > 1) {
         constexpr int rows = kMergeThreads / 64;
@@ -406,12 +466,27 @@ specpv_status launch_typed(const AttnArgs& a, SimtParams& p, cudaStream_t stream
     return SPECPV_OK;
 }
 
+template <bool kQ4>
+specpv_status launch_for_cache(const AttnArgs& a, SimtParams& p, cudaStream_t stream) {
+    if (a.g.dtype == SPECPV_DTYPE_F32) {
+        if (a.g.d == 64) return launch_typed<float, float, 64, kQ4>(a, p, stream);
+        if (a.g.d == 128) return launch_typed<float, float, 128, kQ4>(a, p, stream);
+    } else if (a.g.out_f32) {
+        if (a.g.d == 64) return launch_typed<__nv_bfloat16, float, 64, kQ4>(a, p, stream);
+        if (a.g.d == 128) return launch_typed<__nv_bfloat16, float, 128, kQ4>(a, p, stream);
+    } else {
+        if (a.g.d == 64) return launch_typed<__nv_bfloat16, __nv_bfloat16, 64, kQ4>(a, p, stream);
+        if (a.g.d == 128) return launch_typed<__nv_bfloat16, __nv_bfloat16, 128, kQ4>(a, p, stream);
+    }
+    return SPECPV_ERR_SHAPE;
+}
+
 }  // namespace
 
 specpv_status launch_attention_simt(const AttnArgs& a, cudaStream_t stream) {
     SimtParams p{};
     p.q = a.q; p.k_new = a.k_new; p.v_new = a.v_new; p.tree_mask = a.tree_mask; p.q_lens = a.q_lens;
-    p.k_pool = a.k_pool; p.v_pool = a.v_pool; p.block_table = a.block_table; p.seq_lens = a.seq_lens;
+    p.k_pool = a.k_pool; p.v_pool = a.v_pool; p.q4_pool = a.q4_pool; p.block_table = a.block_table; p.seq_lens = a.seq_lens;
     p.out = a.out; p.lse = a.lse; p.workspace = a.workspace;
     p.layer0 = a.layer0; p.batch = a.batch; p.M_max = a.M_max; p.mask_words = a.mask_words;
     p.Hq = a.g.Hq; p.Hkv = a.g.Hkv; p.G = a.g.G; p.bs = a.g.bs; p.max_blocks = a.max_blocks; p.n_pages = a.n_pages;
@@ -436,17 +511,7 @@ specpv_status launch_attention_simt(const AttnArgs& a, cudaStream_t stream) {
     p.part_o = reinterpret_cast<float*>(ws);
     p.part_ml = reinterpret_cast<float*>(ws + (size_t)base * n_splits * R_max * a.g.d * sizeof(float));
 
-    if (a.g.dtype == SPECPV_DTYPE_F32) {
-        if (a.g.d == 64) return launch_typed<float, float, 64>(a, p, stream);
-        if (a.g.d == 128) return launch_typed<float, float, 128>(a, p, stream);
-    } else if (a.g.out_f32) {
-        if (a.g.d == 64) return launch_typed<__nv_bfloat16, float, 64>(a, p, stream);
-        if (a.g.d == 128) return launch_typed<__nv_bfloat16, float, 128>(a, p, stream);
-    } else {
-        if (a.g.d == 64) return launch_typed<__nv_bfloat16, __nv_bfloat16, 64>(a, p, stream);
-        if (a.g.d == 128) return launch_typed<__nv_bfloat16, __nv_bfloat16, 128>(a, p, stream);
-    }
-    return SPECPV_ERR_SHAPE;
+    return a.q4_pool ? launch_for_cache<true>(a, p, stream) : launch_for_cache<false>(a, p, stream);
 }
 
 }  // namespace specpv

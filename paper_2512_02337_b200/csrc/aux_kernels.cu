@@ -317,7 +317,7 @@ __global__ void __launch_bounds__(kSelectThreads, kSelectThreads == 512 && kSele
         return acc * inv_heads;
     };
     const int count = min(nb, p.budget_blocks);
-    if (l == 0 && h == 0 && tid == 0) p.count[b] = count;
+    if (p.count && l == 0 && h == 0 && tid == 0) p.count[b] = count;
     if (nb <= p.budget_blocks) {
         for (int i = tid; i < nb; i += kSelectThreads) idx[i] = i;
         return;

@@ -35,7 +35,7 @@ struct SelectParams {
     const float* scores;
     const int32_t* seq_lens;
     int32_t* idx;
-    int32_t* count;
+    int32_t* count;  // nullable
     int batch, Hkv, bs, max_blocks, sink_blocks, local_blocks, budget_blocks;
     int pdl;          // set by launch_pdl_if
     int share_heads;  // 1: every KV head of a layer keeps the blocks chosen on the mean of the heads' scores
@@ -74,6 +74,67 @@ struct CommitParams {
     int pdl;      // set by launch_pdl_if
 };
 
+// A commit into a cache in 4 bits (cache_q4.cu).
+struct CommitQ4Params {
+    const void* k_new;
+    const void* v_new;
+    const int32_t* accepted;  // nullable: rows 0 .. n - 1
+    const int32_t* n_accepted;
+    void* pool;
+    const int32_t* block_table;
+    int32_t* seq_lens;
+    void* kmax;  // nullable, with kmin
+    void* kmin;
+    void* k_values;  // nullable: what the appended rows stand for, [layers in call][batch][A_max][Hkv][d]
+    void* v_values;
+    void* workspace;
+    int layer0, batch, M_max, A_max, Hkv, bs, max_blocks, n_pages;
+    int pdl;  // set by launch_pdl_if
+};
+
+// A gather out of a cache in 4 bits (cache_q4.cu).
+struct GatherQ4Params {
+    const void* pool;
+    const int32_t* full_table;
+    const int32_t* seq_lens;
+    const int32_t* idx;
+    const int32_t* count;
+    void* part_k;
+    void* part_v;
+    const int32_t* part_table;
+    int32_t* partial_lens;
+    void* workspace;
+    int batch, Hkv, bs, budget_blocks, full_max_blocks, full_pages, part_max_blocks, part_pages;
+    int pdl;  // set by launch_pdl_if
+};
+
+// The account of attention weight, and eviction by it (evict.cu).
+struct AccumulateParams {
+    const void* q;
+    const float* lse;
+    const int32_t* accepted;  // nullable: rows 0 .. n - 1
+    const int32_t* n_accepted;
+    const void* k_pool;
+    const int32_t* block_table;
+    const int32_t* seq_lens;
+    float* acc;
+    void* workspace;
+    int layer0, batch, M_max, A_max, Hq, Hkv, G, bs, max_blocks, n_pages;
+    float scale;
+    int pdl;  // set by launch_pdl_if
+};
+struct EvictParams {
+    void* k_pool;
+    void* v_pool;
+    const int32_t* block_table;
+    int32_t* seq_lens;
+    float* acc;
+    const int32_t* idx;  // kept tokens of every (layer, sequence, KV head), ascending
+    void* workspace;
+    int batch, Hkv, bs, row_bytes, keep, max_blocks, n_pages;
+    int pdl;  // set by launch_pdl_if
+};
+
 specpv_status launch_summaries(const SummaryParams& p, int n_layers, int blocks_touched, int dtype, cudaStream_t stream);
 specpv_status launch_scores(const ScoreParams& p, int n_layers, int max_nb, int dtype, int d, cudaStream_t stream);
 bool scores_tc_supported(const ScoreParams& p, int dtype, int d);
@@ -83,5 +144,9 @@ specpv_status launch_select(const SelectParams& p, int n_layers, cudaStream_t st
 specpv_status launch_gather(const GatherParams& p, int n_layers, cudaStream_t stream);
 // advance: this call holds the model's last layer, the lengths advance
 specpv_status launch_commit(const CommitParams& p, int n_layers, int dtype, bool advance, cudaStream_t stream);
+specpv_status launch_commit_q4(const CommitQ4Params& p, int n_layers, int dtype, int d, bool advance, cudaStream_t stream);
+specpv_status launch_gather_q4(const GatherQ4Params& p, int n_layers, int dtype, int d, cudaStream_t stream);
+specpv_status launch_accumulate(const AccumulateParams& p, int n_layers, int max_seq_len, int dtype, int d, cudaStream_t stream);
+specpv_status launch_evict(const EvictParams& p, int n_layers, cudaStream_t stream);
 
 }  // namespace specpv

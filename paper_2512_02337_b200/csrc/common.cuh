@@ -148,6 +148,7 @@ struct AttnArgs {
     const int32_t* q_lens;
     const void* k_pool;
     const void* v_pool;
+    const void* q4_pool;  // a cache in 4 bits instead of k_pool and v_pool
     const int32_t* block_table;
     const int32_t* seq_lens;
     int max_blocks, n_pages, max_seq_len;

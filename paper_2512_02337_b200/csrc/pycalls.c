@@ -13,7 +13,8 @@
 #include "../../include/specpv.h"
 
 /* Argument kinds: G specpv_config structure, i int, P tensor or None, C cache (the binding's Cache, or anything else whose
- * desc() gives a specpv_paged_kv structure) -> specpv_paged_kv, W workspace tensor -> pointer and bytes, S stream or None (the
+ * desc() gives a specpv_paged_kv structure) -> specpv_paged_kv, Q cache in 4 bits (anything whose desc() gives a specpv_paged_q4
+ * structure) -> specpv_paged_q4, W workspace tensor -> pointer and bytes, S stream or None (the
  * current one). */
 typedef struct {
     const char *name, *kinds;
@@ -56,6 +57,23 @@ static int call_qkv(const uint64_t *v) {
 }
 static int call_o_proj(const uint64_t *v) {
     return specpv_o_proj(P(0), I(1), I(2), P(3), P(4), I(5), P(6), I(7), I(8), P(9), P(10), (size_t)v[11], P(12));
+}
+
+static int call_verify_q4(const uint64_t *v) {
+    return specpv_verify_full_q4(P(0), I(1), I(2), P(3), P(4), P(5), P(6), P(7), I(8), P(9), P(10), P(11), P(12), (size_t)v[13], P(14));
+}
+static int call_commit_q4(const uint64_t *v) {
+    return specpv_commit_accepted_q4(P(0), I(1), I(2), P(3), P(4), I(5), P(6), P(7), I(8), P(9), P(10), P(11), P(12), P(13), P(14),
+                                     (size_t)v[15], P(16));
+}
+static int call_refresh_q4(const uint64_t *v) {
+    return specpv_refresh_partial_q4(P(0), P(1), P(2), P(3), P(4), P(5), P(6), (size_t)v[7], P(8));
+}
+static int call_accumulate(const uint64_t *v) {
+    return specpv_accumulate_attention(P(0), I(1), I(2), P(3), P(4), I(5), P(6), P(7), I(8), P(9), P(10), P(11), (size_t)v[12], P(13));
+}
+static int call_evict(const uint64_t *v) {
+    return specpv_evict_tokens(P(0), P(1), P(2), I(3), I(4), I(5), P(6), P(7), (size_t)v[8], P(9));
 }
 
 /* set once by init(): torch.Tensor, the binding's converters, torch's current device and stream, the binding's Cache and
@@ -146,6 +164,15 @@ static int cache_of(PyObject *cache, specpv_paged_kv *kv) {
     return st;
 }
 
+static int q4_of(PyObject *cache, specpv_paged_q4 *kv) {
+    const void *desc = NULL;
+    PyObject *d = PyObject_CallMethodNoArgs(cache, s_desc);
+    const int bad = !d || structure_of(d, sizeof *kv, &desc);
+    if (!bad) *kv = *(const specpv_paged_q4 *)desc;
+    Py_XDECREF(d);
+    return bad ? -1 : 0;
+}
+
 static int config_of(PyObject *arg, uint64_t *out) {
     const void *cfg = NULL;
     if (structure_of(arg, sizeof(specpv_config), &cfg)) return -1;
@@ -177,6 +204,7 @@ static int stream_of(PyObject *arg, uint64_t *out) {
 static PyObject *invoke(const Spec *spec, PyObject *const *args, Py_ssize_t n) {
     uint64_t v[kMaxValues];
     specpv_paged_kv caches[kMaxCaches];
+    specpv_paged_q4 q4;  /* one to a call */
     int n_v = 0, n_caches = 0;
     if (n != (Py_ssize_t)strlen(spec->kinds) || !tensor_type) {
         PyErr_Format(PyExc_TypeError, "%s: wrong number of arguments", spec->name);
@@ -190,6 +218,10 @@ static PyObject *invoke(const Spec *spec, PyObject *const *args, Py_ssize_t n) {
             case 'C':
                 st = cache_of(args[i], &caches[n_caches]);
                 v[n_v] = (uint64_t)(uintptr_t)&caches[n_caches++];
+                break;
+            case 'Q':
+                st = q4_of(args[i], &q4);
+                v[n_v] = (uint64_t)(uintptr_t)&q4;
                 break;
             case 'S': st = stream_of(args[i], &v[n_v]); break;
             case 'W':
@@ -219,7 +251,12 @@ static PyObject *invoke(const Spec *spec, PyObject *const *args, Py_ssize_t n) {
     X(specpv_verify_host, "GiiiPPPPiCPPWS", call_verify_host)           \
     X(specpv_commit_accepted, "GiiPPiPPiCPPWS", call_commit)            \
     X(specpv_qkv_rope, "GiiPiPPiiPPPWS", call_qkv)                      \
-    X(specpv_o_proj, "GiiPPiPiiPWS", call_o_proj)
+    X(specpv_o_proj, "GiiPPiPiiPWS", call_o_proj)                       \
+    X(specpv_verify_full_q4, "GiiPPPPPiQPPWS", call_verify_q4)          \
+    X(specpv_commit_accepted_q4, "GiiPPiPPiQPPPPWS", call_commit_q4)    \
+    X(specpv_refresh_partial_q4, "GQPPCPWS", call_refresh_q4)           \
+    X(specpv_accumulate_attention, "GiiPPiPPiCPWS", call_accumulate)    \
+    X(specpv_evict_tokens, "GCPiiiPWS", call_evict)
 
 #define WRAPPER(name, kinds, call)                                                       \
     static PyObject *py_##name(PyObject *self, PyObject *const *args, Py_ssize_t n) {    \
