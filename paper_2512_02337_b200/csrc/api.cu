@@ -635,7 +635,8 @@ SPECPV_EXPORT specpv_status specpv_verify_full_q4(const specpv_config* cfg, int 
     a.out = out; a.lse = lse; a.workspace = workspace;
     a.partial_off = w.partial_off;
     a.partial_bytes = w.partial_bytes;
-    return launch_attention_simt(a, reinterpret_cast<cudaStream_t>(stream));
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    return attention_tc_supported(a) ? launch_attention_tc(a, s) : launch_attention_simt(a, s);
 }
 
 SPECPV_EXPORT specpv_status specpv_commit_accepted_q4(const specpv_config* cfg, int layer0, int n_layers, const void* k_new,

@@ -450,6 +450,15 @@ __global__ void __launch_bounds__(kMergeThreads) merge_splits_kernel(SimtParams 
     if (p.lse && lane == 0) p.lse[row] = m_all + logf(l_all);
 }
 
+template <typename TO, int D>
+specpv_status launch_merge(const AttnArgs& a, SimtParams& p, cudaStream_t stream) {
+    constexpr int rows = kMergeThreads / 64;
+    dim3 mgrid((a.M_max * a.g.G + rows - 1) / rows, a.g.Hkv, a.n_layers * a.batch);
+    if (launch_pdl_if(merge_splits_kernel<TO, D>, mgrid, kMergeThreads, 0, stream, p) != cudaSuccess) return SPECPV_ERR_CUDA;
+    count_launch();
+    return SPECPV_OK;
+}
+
 template <typename T, typename TO, int D, bool kQ4>
 specpv_status launch_typed(const AttnArgs& a, SimtParams& p, cudaStream_t stream) {
     constexpr size_t smem = simt_smem<D>();
@@ -457,13 +466,7 @@ specpv_status launch_typed(const AttnArgs& a, SimtParams& p, cudaStream_t stream
     dim3 grid(p.n_splits * p.row_tiles, a.g.Hkv, a.n_layers * a.batch);
     if (launch_pdl_if(attn_simt_kernel<T, TO, D, kQ4>, grid, kThreads, smem, stream, p) != cudaSuccess) return SPECPV_ERR_CUDA;
     count_launch();
-    if (p.n_splits > 1) {
-        constexpr int rows = kMergeThreads / 64;
-        dim3 mgrid((a.M_max * a.g.G + rows - 1) / rows, a.g.Hkv, a.n_layers * a.batch);
-        if (launch_pdl_if(merge_splits_kernel<TO, D>, mgrid, kMergeThreads, 0, stream, p) != cudaSuccess) return SPECPV_ERR_CUDA;
-        count_launch();
-    }
-    return SPECPV_OK;
+    return p.n_splits > 1 ? launch_merge<TO, D>(a, p, stream) : SPECPV_OK;
 }
 
 template <bool kQ4>
@@ -483,7 +486,7 @@ specpv_status launch_for_cache(const AttnArgs& a, SimtParams& p, cudaStream_t st
 
 }  // namespace
 
-specpv_status launch_attention_simt(const AttnArgs& a, cudaStream_t stream) {
+static SimtParams simt_params(const AttnArgs& a) {
     SimtParams p{};
     p.q = a.q; p.k_new = a.k_new; p.v_new = a.v_new; p.tree_mask = a.tree_mask; p.q_lens = a.q_lens;
     p.k_pool = a.k_pool; p.v_pool = a.v_pool; p.q4_pool = a.q4_pool; p.block_table = a.block_table; p.seq_lens = a.seq_lens;
@@ -491,6 +494,18 @@ specpv_status launch_attention_simt(const AttnArgs& a, cudaStream_t stream) {
     p.layer0 = a.layer0; p.batch = a.batch; p.M_max = a.M_max; p.mask_words = a.mask_words;
     p.Hq = a.g.Hq; p.Hkv = a.g.Hkv; p.G = a.g.G; p.bs = a.g.bs; p.max_blocks = a.max_blocks; p.n_pages = a.n_pages;
     p.scale = a.g.scale;
+    return p;
+}
+
+specpv_status launch_merge_splits(const AttnArgs& a, int n_splits, float* part_o, float* part_ml, cudaStream_t stream) {
+    SimtParams p = simt_params(a);
+    p.n_splits = n_splits; p.part_o = part_o; p.part_ml = part_ml;
+    if (a.g.d == 64) return a.g.out_f32 ? launch_merge<float, 64>(a, p, stream) : launch_merge<__nv_bfloat16, 64>(a, p, stream);
+    return a.g.out_f32 ? launch_merge<float, 128>(a, p, stream) : launch_merge<__nv_bfloat16, 128>(a, p, stream);
+}
+
+specpv_status launch_attention_simt(const AttnArgs& a, cudaStream_t stream) {
+    SimtParams p = simt_params(a);
 
     // split the KV range so that the launch has up to 296 CTAs, down to one tile per CTA (a tile takes some 3 us, a partial result a
     // fraction of one), as far as the workspace allows: two CTAs per SM with 64 channels; with 128, where shared memory

@@ -34,6 +34,7 @@
 // (4101 tokens, 60 x 4 rows of 64).  It takes half again the contractions of P V and a third more of the softmax: 24.6 -> 31.4 us and
 // 16.1 -> 18.7 us for one layer, where the plain kernel took 1310 and 375.
 #include "attn_tc.cuh"
+#include "q4.cuh"
 
 namespace specpv {
 
@@ -46,15 +47,18 @@ constexpr int kThreadsTc = 384;          // 12 warps
 // split into groups of eight).  (The copy engine spends some 60 ns per box whatever it carries, and a copy per page and part
 // made 16-token pages wait for it: 61440 tokens x 16 layers, 32 rows,
 // 834 -> 675 us; a copy of half a page or a quarter is no faster.)
-template <int D>
+// kQ4 gives up a slot for two stages of codes (a tile's key and value codes; scales and offsets of its values).
+template <int D, bool kQ4 = false>
 struct Shape {
     static constexpr int kParts = D / 64;
     static constexpr int kSlotBytes = kTileTokens * D * 2;
-    static constexpr int kStages = D == 128 ? 5 : 10;
+    static constexpr int kStages = (D == 128 ? 5 : 10) - (kQ4 ? 1 : 0);
+    static constexpr int kCodeStages = kQ4 ? 2 : 0;
+    static constexpr int kCodeBytes = kTileTokens * D, kParamBytes = kTileTokens * 4;
     static constexpr int kGroupBytes = 8 * D * 2;  // eight tokens of a K or V tile
     static constexpr int kQTileBytes = 128 * D * 2;
     static constexpr int kQBytes = 2 * kQTileBytes;
-    static constexpr int kSmemBytes = 1024 + kQBytes + kStages * kSlotBytes;
+    static constexpr int kSmemBytes = 1024 + kQBytes + kStages * kSlotBytes + kCodeStages * (kCodeBytes + kParamBytes);
 };
 constexpr int kMaxStages = 10;
 constexpr int kShortWalk = 4;  // tiles per CTA
@@ -80,6 +84,8 @@ struct __align__(8) Barriers {
     uint64_t drain;             // completion of the contractions issued before a wait gave up
     uint32_t tmem_base;
     int abort_flag;
+    int odd;                    // kQ4: an infinity or NaN among the step's own values
+    uint64_t code_full[2], code_empty[2];  // kQ4: the codes of a tile have landed, have been opened
 };
 
 // What every role of a CTA knows about its work.
@@ -173,15 +179,221 @@ __device__ __forceinline__ void produce(const TcParams& p, const Job& c, Barrier
     }
 }
 
+// =========================== a cache in 4 bits (kQ4) ======================================
+// The producer copies a tile's codes, two copies per page, and eight more warps open them to bfloat16 into the ring, where the tensor
+// maps would have delivered them.
+template <int D>
+__device__ __forceinline__ void produce_codes(const TcParams& p, const Job& c, Barriers& bars, int lane) {
+    using Sh = Shape<D, true>;
+    const int ppt = kTileTokens / p.bs;
+    const uint32_t page_bytes = (uint32_t)q4::page_bytes(p.bs, D), code_bytes = (uint32_t)p.bs * D, param_bytes = (uint32_t)p.bs * 4;
+    const char* pool = reinterpret_cast<const char*>(p.q4_pool) + ((size_t)(p.layer0 + c.l) * p.n_pages * p.Hkv + c.h) * page_bytes;
+    const int32_t* table = p.block_table + (size_t)c.b * p.max_blocks;
+    const uint32_t codes = c.q_smem + Sh::kQBytes + Sh::kStages * Sh::kSlotBytes, params = codes + Sh::kCodeStages * Sh::kCodeBytes;
+    auto entry_of = [&](int j) {  // of the lane's page; looked at when it is used, a tile later
+        const int blk = (c.tile_begin + j) * ppt + lane;
+        return lane >= ppt || j >= c.n_ctx_tiles || (long long)blk * p.bs >= c.seq_len || blk >= p.max_blocks ? -1 : table[blk];
+    };
+    // (a page is also asked for in L2 kAhead tiles before it is copied: two stages alone do not cover the latency of HBM)
+    constexpr int kAhead = 4;
+    int entry[kAhead + 1];
+#pragma unroll
+    for (int j = 0; j <= kAhead; ++j) entry[j] = entry_of(j);
+    for (int j = 0; j < c.n_ctx_tiles; ++j) {
+        const uint32_t stage = j & 1, full = smem_u32(&bars.code_full[stage]);
+        const int page = entry[0];
+        const bool there = page >= 0 && page < p.n_pages;
+        const int blk = (c.tile_begin + j) * ppt + lane;
+        if (!there && lane < ppt && (long long)blk * p.bs < c.seq_len && blk < p.max_blocks)
+            record_fault(p.workspace, SPECPV_ERR_BAD_BLOCK_TABLE, c.b, blk, page, c.l);
+        const char* ahead = pool + (size_t)entry[kAhead] * p.Hkv * page_bytes;
+        if (entry[kAhead] >= 0 && entry[kAhead] < p.n_pages)
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(ahead), "r"(page_bytes) : "memory");
+#pragma unroll
+        for (int x = 0; x < kAhead; ++x) entry[x] = entry[x + 1];
+        entry[kAhead] = entry_of(j + kAhead + 1);
+        if (j >= 2 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.code_empty[stage]), ((j >> 1) + 1) & 1, &bars.abort_flag, p.workspace, 12)))
+            break;
+        const uint32_t n_pages = (uint32_t)__popc(__ballot_sync(0xffffffffu, there));
+        if (lane == 0) mbar_expect_tx(full, n_pages * (code_bytes + param_bytes));
+        __syncwarp();
+        if (there) {
+            const char* src = pool + (size_t)page * p.Hkv * page_bytes;
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                         ::"r"(codes + stage * Sh::kCodeBytes + lane * code_bytes), "l"(src), "r"(code_bytes), "r"(full) : "memory");
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                         ::"r"(params + stage * Sh::kParamBytes + lane * param_bytes), "l"(src + code_bytes + param_bytes), "r"(param_bytes), "r"(full) : "memory");
+        }
+        __syncwarp();
+    }
+}
+
+// Four warps open the K tiles, four the V tiles (one warp per scheduler waits for its own results: with four for both, a tile took
+// 4200 cycles, its contractions 1350).  A thread owns a token of a K tile (16 bytes of codes of 32 channels at a time), and eight
+// channels of 16 (8 with 64 channels) tokens of a V tile, whose pairs of tokens become pairs of channels in registers.  V rows past
+// the valid tokens, and what is behind a bad page id, become zeros here.
+template <int D, bool kV>
+__device__ __forceinline__ void open_tiles(const TcParams& p, const Job& c, Barriers& bars, bool one, int tid) {
+    using Sh = Shape<D, true>;
+    constexpr int kVTok = D / 8;  // tokens of a V tile per thread
+    const int lane = tid & 31;
+    const uint32_t ring = c.q_smem + Sh::kQBytes, codes = ring + Sh::kStages * Sh::kSlotBytes, params = codes + Sh::kCodeStages * Sh::kCodeBytes;
+    const int ppt = kTileTokens / p.bs;
+    const int cg = tid % (D / 8), t0 = kV ? tid / (D / 8) * kVTok : tid;  // first token
+    const int at_page = t0 % p.bs, page_in_tile = t0 / p.bs;
+    // within a stage: pages of bs D bytes of codes and 4 bs bytes of value scales and offsets
+    const uint32_t my_codes = codes + page_in_tile * p.bs * D + (kV ? q4::v_word(p.bs, D, at_page, cg * 8) * 4 : at_page * 16);
+    const uint32_t my_params = params + page_in_tile * p.bs * 4 + at_page * 2, two_bs = 2u * p.bs;
+    const char* k_params = reinterpret_cast<const char*>(p.q4_pool) + ((size_t)(p.layer0 + c.l) * p.n_pages * p.Hkv + c.h) * q4::page_bytes(p.bs, D) +
+                           q4::param_at(p.bs, D, 0, at_page) * 2;
+    const uint32_t page_stride = (uint32_t)(p.Hkv * q4::page_bytes(p.bs, D));
+    const int32_t* table = p.block_table + (size_t)c.b * p.max_blocks;
+    auto entry_of = [&](int j) {  // of the thread's page of tile j
+        const int blk = (c.tile_begin + j) * ppt + page_in_tile;
+        return j >= c.n_ctx_tiles || (long long)blk * p.bs >= c.seq_len || blk >= p.max_blocks ? -1 : table[blk];
+    };
+    auto is_page = [&](int entry) { return entry >= 0 && entry < p.n_pages; };
+    // a key's scale and offset come straight from memory, a tile ahead
+    uint32_t scale_next = 0, offset_next = 0;
+    auto fetch_params = [&](int entry) {
+        scale_next = offset_next = 0;
+        if (kV || !is_page(entry)) return;
+        const char* base = k_params + (size_t)entry * page_stride;
+        scale_next = *reinterpret_cast<const uint16_t*>(base);
+        offset_next = *reinterpret_cast<const uint16_t*>(base + two_bs);
+    };
+    int entry = entry_of(kV ? 0 : 1);  // V: of tile j; K: of tile j + 1
+    if (!kV) fetch_params(entry_of(0));
+
+    auto store16 = [](uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+    };
+    auto load16 = [](uint32_t at) {
+        uint4 v;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+        return v;
+    };
+    auto load4 = [](uint32_t at) {
+        uint32_t v;
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+        return v;
+    };
+#pragma unroll 1
+    for (int j = 0; j < c.n_tiles; ++j) {
+        const bool step = j >= c.n_ctx_tiles;
+        const uint32_t stage = j & 1;
+        // ring uses: K0 V0 K1 V1 .. with two row tiles, K0 K1 V0 K2 V1 K3 .. with one
+        const int use = !one ? 2 * j + kV : kV ? (j < c.n_tiles - 1 ? 2 * j + 2 : 2 * j + 1) : max(2 * j - 1, 0);
+        const uint32_t slot = (uint32_t)use % Sh::kStages, round = (uint32_t)use / Sh::kStages;
+        bool ok = true;
+        if (!step) ok = mbar_wait(smem_u32(&bars.code_full[stage]), (j >> 1) & 1, &bars.abort_flag, p.workspace, 13);
+        if (round) ok &= mbar_wait(smem_u32(&bars.kv_empty[slot]), (round + 1) & 1, &bars.abort_flag, p.workspace, 11);
+        if (!__all_sync(0xffffffffu, ok)) return;
+        const uint32_t dst = ring + slot * Sh::kSlotBytes;
+        if (step) {
+            // the step's own tokens, 16 bytes at a time, rows past them zero; values that are infinite or NaN go another way
+            const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(kV ? p.v_new : p.k_new) +
+                                                              ((size_t)c.lb * p.M_max * p.Hkv + c.h) * D);
+            bool found = false;
+#pragma unroll 2
+            for (int x = tid; x < kTileTokens * (D / 8); x += 128) {
+                const int t = x / (D / 8), chunk = x % (D / 8);
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (t < c.M) v = src[(size_t)t * p.Hkv * (D / 8) + chunk];
+                if (kV) {
+                    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const bool lo = (w[y] & 0x7F80u) == 0x7F80u, hi = (w[y] & 0x7F800000u) == 0x7F800000u;
+                        found |= lo | hi;
+                        w[y] &= (lo ? 0xFFFF0000u : ~0u) & (hi ? 0xFFFFu : ~0u);
+                    }
+                    v = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+                store16(dst + (t >> 3) * Sh::kGroupBytes + (chunk >> 3) * 1024 + (t & 7) * 128 + (((chunk & 7) ^ (t & 7)) << 4), v.x, v.y, v.z, v.w);
+            }
+            if (found) bars.odd = 1;
+        } else if (!kV) {
+            const uint32_t scale = scale_next * 0x10001u, offset = offset_next * 0x10001u;
+            fetch_params(entry);
+            entry = entry_of(j + 2);
+            const uint32_t at = my_codes + stage * Sh::kCodeBytes, row = dst + (tid >> 3) * Sh::kGroupBytes + (tid & 7) * 128;
+            const uint32_t low = (tid & 3) << 4, high = (tid & 4) << 4;  // the swizzle's bits
+#pragma unroll 1
+            for (int x = 0; x < D / 32; ++x) {
+                const uint4 q = load16(at + x * p.bs * 16);
+                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+                const uint32_t to = row + (x >> 1) * 1024 + (((x & 1) << 6) ^ high);
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    store16(to + ((y << 4) ^ low), q4::fma_bf16x2(q4::open_pair(w[y], 0), scale, offset), q4::fma_bf16x2(q4::open_pair(w[y], 1), scale, offset),
+                            q4::fma_bf16x2(q4::open_pair(w[y], 2), scale, offset), q4::fma_bf16x2(q4::open_pair(w[y], 3), scale, offset));
+            }
+        } else {
+            const int left = is_page(entry) ? c.seq_len - (c.tile_begin + j) * kTileTokens - t0 : 0;  // valid tokens of the thread's
+            entry = entry_of(j + 1);
+            const uint32_t at = my_codes + stage * Sh::kCodeBytes, pat = my_params + stage * Sh::kParamBytes;
+            const uint32_t col = dst + (cg >> 3) * 1024;
+            uint32_t words[kVTok / 8][8];  // of eight tokens of each channel
+            if constexpr (D == 128) {  // (64 bytes a thread; one word at a time 16 lanes would meet in a bank)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const uint4 q = load16(at + x * 16);
+                    words[0][2 * x] = q.x; words[1][2 * x] = q.y; words[0][2 * x + 1] = q.z; words[1][2 * x + 1] = q.w;
+                }
+            } else {
+#pragma unroll
+                for (int y = 0; y < 8; ++y) words[0][y] = load4(at + y * 8);
+            }
+#pragma unroll
+            for (int g = 0; g < kVTok / 8; ++g) {
+                uint32_t (&w)[8] = words[g];
+                const uint32_t rows = col + ((t0 >> 3) + g) * Sh::kGroupBytes;
+#pragma unroll 1
+                for (int x = 0; x < 8; x += 4) {  // tokens t0 + 8 g + x .. + 3
+                    uint32_t sc[2], of[2];
+                    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(sc[0]), "=r"(sc[1]) : "r"(pat + g * 16 + x * 2) : "memory");
+                    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(of[0]), "=r"(of[1]) : "r"(pat + two_bs + g * 16 + x * 2) : "memory");
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int n = left - 8 * g - x - 2 * u;
+                        const uint32_t keep = n > 1 ? ~0u : n > 0 ? 0xFFFFu : 0u;  // a token that is not there: no scale, no offset, no value
+                        sc[u] &= keep;
+                        of[u] &= keep;
+                        uint32_t even[4], odd[4];
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {  // channels 2 y and 2 y + 1 of the eight
+                            const uint32_t a = q4::fma_bf16x2(q4::open_pair(w[2 * y], u), sc[u], of[u]), z = q4::fma_bf16x2(q4::open_pair(w[2 * y + 1], u), sc[u], of[u]);
+                            even[y] = __byte_perm(a, z, 0x5410);
+                            odd[y] = __byte_perm(a, z, 0x7632);
+                        }
+                        const int t = x + 2 * u;
+                        store16(rows + t * 128 + (((cg & 7) ^ t) << 4), even[0], even[1], even[2], even[3]);
+                        store16(rows + t * 128 + 128 + (((cg & 7) ^ (t + 1)) << 4), odd[0], odd[1], odd[2], odd[3]);
+                    }
+#pragma unroll
+                    for (int y = 0; y < 8; ++y) w[y] = __funnelshift_r(w[y], w[y], 8);
+                }
+            }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            mbar_arrive(smem_u32(&bars.kv_full[slot]));
+            if (!step) mbar_arrive(smem_u32(&bars.code_empty[stage]));
+        }
+    }
+}
+
 // =========================== MMA issuer ==================================================
 // One warp issues every contraction (issuing from two warps serialises the tensor pipe).  Issue
 // order (ping-pong of the two streams): QK(0,0) QK(0,1) | PV(0,0) QK(1,0) PV(0,1) QK(1,1) | ...
 // Barrier instructions do not overlap with queued MMAs (each costs the pipe 30-100 idle cycles),
 // so the loop keeps them to four waits per KV tile, without votes, and four commits behind MMAs.  The whole
 // warp runs the loop, lane 0 issues.
-template <int D, bool kOne, bool kSplit>
+template <int D, bool kOne, bool kSplit, bool kQ4>
 __device__ __forceinline__ void issue(const TcParams& p, const Job& c, Barriers& bars, int lane) {
-    using Sh = Shape<D>;
+    using Sh = Shape<D, kQ4>;
     constexpr int kStages = Sh::kStages;
     constexpr uint32_t kSlotWords = Sh::kSlotBytes >> 4, kQTileWords = Sh::kQTileBytes >> 4;  // 16-byte units of descriptors
     volatile int* abort_flag = &bars.abort_flag;
@@ -365,7 +577,7 @@ __device__ __noinline__ void pass_zeros(const TcParams& p, Barriers& bars, int t
     mbar_wait(smem_u32(&bars.o_done[t]), 0, abort_flag, p.workspace, 8);  // its contractions have ended before the CTA does
 }
 
-template <int D, bool kOne, bool kSplit>
+template <int D, bool kOne, bool kSplit, bool kQ4>
 __device__ __forceinline__ void softmax(const TcParams& p, const Job& c, Barriers& bars, int warp, int lane) {
     using Sh = Shape<D>;
     volatile int* abort_flag = &bars.abort_flag;
@@ -476,6 +688,9 @@ __device__ __forceinline__ void softmax(const TcParams& p, const Job& c, Barrier
                     const float2 r = __ffma2_rn(e, make_float2(kOnePlus, kOnePlus), minus_upper);
                     rest[i] = pack_bf16(r.x, r.y);
                     sum2[i & 3] = __fadd2_rn(sum2[i & 3], e);
+                } else if constexpr (kQ4) {  // over the float32 weights: the log-sum-exp is accurate to float32
+                    v[i] = pack_bf16(e.x, e.y);
+                    sum2[i & 3] = __fadd2_rn(sum2[i & 3], e);
                 } else {
                     const uint32_t w = pack_bf16(e.x, e.y);
                     v[i] = w;
@@ -535,7 +750,7 @@ __device__ __forceinline__ void softmax(const TcParams& p, const Job& c, Barrier
                 const float factor = !need ? 1.f : (m_run == -INFINITY ? 0.f : ex2(m_run - m_tile));
                 // O_t already holds every earlier PV of this stream: the tensor pipe runs in order, and S_t, issued
                 // after them, is complete
-#pragma unroll (kOne ? 1 : D / 32)
+#pragma unroll (kOne || kQ4 ? 1 : D / 32)
                 for (int cc = 0; cc < D / 32; ++cc) {
                     uint32_t o[32];
                     TMEM_LD32(o_addr + cc * 32, o);
@@ -595,13 +810,13 @@ __device__ __forceinline__ void softmax(const TcParams& p, const Job& c, Barrier
     if (!ok) return;
     tc_fence_after();
     const bool direct = p.n_splits == 1;
-    const float inv = direct ? 1.f / l_run : 1.f;
+    const float inv = !direct ? 1.f : kQ4 && l_run == 0.f ? 0.f : 1.f / l_run;  // kQ4: a row that has seen nothing is zero
     w_mine *= inv;
     w_other *= inv;
     const size_t out_row = ((size_t)c.lb * p.M_max + tok) * p.Hq + c.h * p.G + g;
     const size_t prow = (((size_t)c.lb * p.Hkv + c.h) * p.n_splits + c.split) * p.R_pad + c.rg * p.rg_tiles * 128 + row;
     const int c_begin = meet ? t * kHalfD : 0, c_end = meet ? c_begin + kHalfD : D;
-#pragma unroll (kOne ? 1 : D / 32)
+#pragma unroll (kOne || kQ4 ? 1 : D / 32)
     for (int c0 = c_begin; c0 < c_end; c0 += 32) {
         uint32_t v[32];
         TMEM_LD32(o_addr + c0, v);
@@ -615,6 +830,19 @@ __device__ __forceinline__ void softmax(const TcParams& p, const Job& c, Barrier
             tmem_wait_ld();
         }
         if (!row_valid) continue;
+        if constexpr (kQ4) {
+            if (c.n_ctx_tiles < n_tiles && *(volatile int*)&bars.odd) {  // infinite and NaN values of the step's tokens that this row sees
+                const __nv_bfloat16* own = reinterpret_cast<const __nv_bfloat16*>(p.v_new) + ((size_t)c.lb * p.M_max * p.Hkv + c.h) * D + c0;
+                for (int s = 0; s < c.M; ++s) {
+                    if (!((s < 64 ? mask_lo >> s : mask_hi >> (s - 64)) & 1)) continue;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const float x = __bfloat162float(own[(size_t)s * p.Hkv * D + i]);
+                        if (!isfinite(x)) v[i] = __float_as_uint(__uint_as_float(v[i]) + x);
+                    }
+                }
+            }
+        }
         if (!meet && direct) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * inv);
@@ -650,7 +878,9 @@ __device__ __forceinline__ void softmax(const TcParams& p, const Job& c, Barrier
         if (direct) {
             if (p.lse) p.lse[out_row] = fmaf(m_run, kLn2, logf(l_run));
         } else {
-            p.part_ml[prow * 2] = m_run;  // log2 units, unrounded: the merge takes differences of them
+            // log2 units, unrounded: the merge takes differences of them.  (kQ4: a NaN has to survive the merge, which leaves out what has
+            // seen nothing.)
+            p.part_ml[prow * 2] = kQ4 && l_run != l_run ? INFINITY : m_run;
             p.part_ml[prow * 2 + 1] = l_run;
         }
     }
@@ -661,9 +891,10 @@ __device__ __forceinline__ void softmax(const TcParams& p, const Job& c, Barrier
 // kForm: the row groups a launch can meet (a kernel with both forms has twice the code, which a call that follows other
 // kernels pays for in instruction-cache misses).
 enum { kOneTile, kTwoTiles, kBoth };
-template <int D, int kForm, bool kSplit>
-__global__ void __launch_bounds__(kThreadsTc, 1) attn_tc_kernel(const __grid_constant__ TcParams p) {
-    using Sh = Shape<D>;
+// kQ4: the cache is one in 4 bits; eight more warps (open_tiles) fill the ring.
+template <int D, int kForm, bool kSplit, bool kQ4>
+__global__ void __launch_bounds__(kQ4 ? kThreadsTc + 256 : kThreadsTc, 1) attn_tc_kernel(const __grid_constant__ TcParams p) {
+    using Sh = Shape<D, kQ4>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ Barriers bars;
     Job c;
@@ -695,7 +926,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_tc_kernel(const __grid_con
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&bars.q_full), 1);
         for (int s = 0; s < Sh::kStages; ++s) {
-            mbar_init(smem_u32(&bars.kv_full[s]), 1);
+            mbar_init(smem_u32(&bars.kv_full[s]), kQ4 ? 4 : 1);
             mbar_init(smem_u32(&bars.kv_empty[s]), 1);
         }
         for (int t = 0; t < 2; ++t) {
@@ -707,15 +938,24 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_tc_kernel(const __grid_con
         mbar_init(smem_u32(&bars.v_fixed), 1);
         mbar_init(smem_u32(&bars.drain), 1);
         bars.abort_flag = 0;
+        if (kQ4) {
+            bars.odd = 0;
+            for (int x = 0; x < 2; ++x) {
+                mbar_init(smem_u32(&bars.code_full[x]), 1);
+                mbar_init(smem_u32(&bars.code_empty[x]), 8);
+            }
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         prefetch_map(&p.tm_q);
-        prefetch_map(&p.tm_kpool);
-        prefetch_map(&p.tm_vpool);
+        if (!kQ4) {
+            prefetch_map(&p.tm_kpool);
+            prefetch_map(&p.tm_vpool);
+        }
     }
     if (c.tile_rows < 128) {  // rows past the packed ones are never copied: finite values, so that their softmax stays quiet
         const int n = (128 - c.tile_rows) * 8;
-        for (int i = threadIdx.x; i < 2 * Sh::kParts * n; i += kThreadsTc)
+        for (int i = threadIdx.x; i < 2 * Sh::kParts * n; i += kQ4 ? kThreadsTc + 256 : kThreadsTc)
             *reinterpret_cast<uint4*>(c.smem + (i / n) * 16384 + c.tile_rows * 128 + (i % n) * 16) = make_uint4(0, 0, 0, 0);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -750,11 +990,11 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_tc_kernel(const __grid_con
     // first tile whose V rows need zeroing past the valid tokens: a ragged last context tile, else the
     // tile of the step's own tokens (fewer than 128), else none
     const bool ragged_ctx = c.n_ctx_tiles > 0 && tile_end == total_tiles && (c.seq_len % kTileTokens) != 0;
-    c.first_fix = ragged_ctx ? c.n_ctx_tiles - 1 : ((last_split && c.M < kTileTokens) ? c.n_ctx_tiles : c.n_tiles);
+    c.first_fix = kQ4 ? c.n_tiles : ragged_ctx ? c.n_ctx_tiles - 1 : ((last_split && c.M < kTileTokens) ? c.n_ctx_tiles : c.n_tiles);
 
     if (work && c.n_tiles == 0) {
         // an empty split: publish (m = -inf, l = 0) so that the merge ignores it
-        for (int r = threadIdx.x; r < p.rg_tiles * 128; r += kThreadsTc) {
+        for (int r = threadIdx.x; r < p.rg_tiles * 128; r += kQ4 ? kThreadsTc + 256 : kThreadsTc) {
             const size_t prow = (((size_t)c.lb * p.Hkv + c.h) * p.n_splits + c.split) * p.R_pad + c.rg * p.rg_tiles * 128 + r;
             p.part_ml[prow * 2] = -INFINITY;
             p.part_ml[prow * 2 + 1] = 0.f;
@@ -762,7 +1002,25 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_tc_kernel(const __grid_con
         work = false;
     }
 
-    if (work) {
+    if constexpr (kQ4) {
+        // Registers: 128 x 48 + 256 x 168 + 256 x 48 are the 640 x 96 of the launch
+        if (work) {
+            if (warp < 4) {
+                asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+                if (warp == 0) {
+                    copy_q<D>(p, c, bars, one, lane);
+                    produce_codes<D>(p, c, bars, lane);
+                }
+                if (warp == 1) one ? issue<D, true, kSplit, true>(p, c, bars, lane) : issue<D, false, kSplit, true>(p, c, bars, lane);
+            } else if (warp >= 12) {
+                asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+                warp < 16 ? open_tiles<D, false>(p, c, bars, one, threadIdx.x - kThreadsTc) : open_tiles<D, true>(p, c, bars, one, threadIdx.x - kThreadsTc - 128);
+            } else {
+                asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+                one ? softmax<D, true, kSplit, true>(p, c, bars, warp, lane) : softmax<D, false, kSplit, true>(p, c, bars, warp, lane);
+            }
+        }
+    } else if (work) {
         // Register budget: the control warpgroup (warps 0-3) gives registers to the two softmax warpgroups: 128 x 56 +
         // 256 x 224 = the 384 x 168 of the launch.
         if (warp == 0) {
@@ -771,7 +1029,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_tc_kernel(const __grid_con
             produce<D>(p, c, bars, one, lane);
         } else if (warp == 1) {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-            one ? issue<D, true, kSplit>(p, c, bars, lane) : issue<D, false, kSplit>(p, c, bars, lane);
+            one ? issue<D, true, kSplit, false>(p, c, bars, lane) : issue<D, false, kSplit, false>(p, c, bars, lane);
         } else if (warp == 2) {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
             one ? fix_v<D, true>(p, c, bars, lane) : fix_v<D, false>(p, c, bars, lane);
@@ -779,7 +1037,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_tc_kernel(const __grid_con
             asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         } else {
             asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
-            one ? softmax<D, true, kSplit>(p, c, bars, warp, lane) : softmax<D, false, kSplit>(p, c, bars, warp, lane);
+            one ? softmax<D, true, kSplit, false>(p, c, bars, warp, lane) : softmax<D, false, kSplit, false>(p, c, bars, warp, lane);
         }
     }
 
@@ -857,7 +1115,7 @@ __global__ void __launch_bounds__(kMergeThreads) merge_tc_kernel(const __grid_co
         }
     }
     const size_t row = ((size_t)lb * p.M_max + j) * p.Hq + h * p.G + g;
-    const float inv = 1.f / l_all;
+    const float inv = p.q4_pool && l_all == 0.f ? 0.f : 1.f / l_all;  // over a cache in 4 bits, a row that has seen nothing is zero
     o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
     if (p.out_f32) {
         reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + row * D)[lane] = o;
@@ -870,24 +1128,24 @@ __global__ void __launch_bounds__(kMergeThreads) merge_tc_kernel(const __grid_co
     if (p.lse && lane == 0) p.lse[row] = fmaf(m_all, kLn2, logf(l_all));
 }
 
-template <int D, int kForm, bool kSplit>
+template <int D, int kForm, bool kSplit, bool kQ4>
 specpv_status launch_form(const TcParams& p, int n_lb, cudaStream_t stream) {
-    using Sh = Shape<D>;
-    if (!set_smem_limit_once(reinterpret_cast<const void*>(attn_tc_kernel<D, kForm, kSplit>), Sh::kSmemBytes)) return SPECPV_ERR_CUDA;
-    if (launch_pdl(attn_tc_kernel<D, kForm, kSplit>, p.n_splits * p.n_row_groups * p.Hkv * n_lb, kThreadsTc, Sh::kSmemBytes, stream, p) !=
-        cudaSuccess)
+    using Sh = Shape<D, kQ4>;
+    if (!set_smem_limit_once(reinterpret_cast<const void*>(attn_tc_kernel<D, kForm, kSplit, kQ4>), Sh::kSmemBytes)) return SPECPV_ERR_CUDA;
+    if (launch_pdl(attn_tc_kernel<D, kForm, kSplit, kQ4>, p.n_splits * p.n_row_groups * p.Hkv * n_lb, kQ4 ? kThreadsTc + 256 : kThreadsTc,
+                   Sh::kSmemBytes, stream, p) != cudaSuccess)
         return SPECPV_ERR_CUDA;
     count_launch();
     return SPECPV_OK;
 }
 
-template <int D, bool kSplit>
+template <int D, bool kSplit, bool kQ4>
 specpv_status launch_kernels(const TcParams& p, int n_lb, cudaStream_t stream) {
     // per-sequence row counts, or a last row group of one tile, can bring both forms into one launch
     const bool both = p.rg_tiles == 2 && (p.q_lens || p.n_full_groups < p.n_row_groups);
-    const specpv_status st = p.rg_tiles == 1 ? launch_form<D, kOneTile, kSplit>(p, n_lb, stream)
-                             : both          ? launch_form<D, kBoth, kSplit>(p, n_lb, stream)
-                                             : launch_form<D, kTwoTiles, kSplit>(p, n_lb, stream);
+    const specpv_status st = p.rg_tiles == 1 ? launch_form<D, kOneTile, kSplit, kQ4>(p, n_lb, stream)
+                             : both          ? launch_form<D, kBoth, kSplit, kQ4>(p, n_lb, stream)
+                                             : launch_form<D, kTwoTiles, kSplit, kQ4>(p, n_lb, stream);
     if (st != SPECPV_OK) return st;
     if (p.n_splits > 1) {
         constexpr int rows = kMergeThreads / (D / 4);
@@ -927,7 +1185,7 @@ bool attention_tc_supported(const AttnArgs& a) {
     if (a.M_max > kMaxQTokens) return false;
     // row coordinates of the pool tensor map must fit in a positive int32
     const unsigned long long rows = (unsigned long long)a.g.n_layers * a.n_pages * a.g.Hkv * (unsigned long long)a.g.bs;
-    if (rows >= 0x7FFFFF00ull) return false;
+    if (!a.q4_pool && rows >= 0x7FFFFF00ull) return false;
     return get_encode_fn() != nullptr;
 }
 
@@ -936,7 +1194,7 @@ specpv_status launch_attention_tc(const AttnArgs& a, cudaStream_t stream) {
     const int G = a.g.G, Hq = a.g.Hq, Hkv = a.g.Hkv;
     const uint64_t d = (uint64_t)a.g.d;
     const uint64_t step_tokens = (uint64_t)a.n_layers * a.batch * a.M_max;
-    const bool pair = attention_pair_wanted(a);
+    const bool pair = !a.q4_pool && attention_pair_wanted(a);
     if (pair) {
         uint64_t dims[3] = {d, (uint64_t)Hq, step_tokens};
         uint64_t strides[2] = {2 * d, (uint64_t)Hq * 2 * d};
@@ -950,7 +1208,8 @@ specpv_status launch_attention_tc(const AttnArgs& a, cudaStream_t stream) {
         uint32_t box[4] = {64, (uint32_t)G, (uint32_t)(128 / G), 1};
         if (!encode_map(&p.tm_q, a.q, 4, dims, strides, box)) return SPECPV_ERR_CUDA;
     }
-    {
+    p.q4_pool = a.q4_pool; p.k_new = a.k_new; p.v_new = a.v_new;
+    if (!a.q4_pool) {
         uint64_t dims[3] = {d, (uint64_t)Hkv, step_tokens};
         uint64_t strides[2] = {2 * d, (uint64_t)Hkv * 2 * d};
         uint32_t box[3] = {64, 1, pair ? 64u : 8u};
@@ -964,7 +1223,7 @@ specpv_status launch_attention_tc(const AttnArgs& a, cudaStream_t stream) {
         uint32_t box[2] = {64, (uint32_t)a.g.bs};
         if (!encode_map(&p.tm_kpool, a.k_pool, 2, dims, strides, box)) return SPECPV_ERR_CUDA;
         if (!encode_map(&p.tm_vpool, a.v_pool, 2, dims, strides, box)) return SPECPV_ERR_CUDA;
-    } else {  // (64 channels, 8 tokens, parts, groups of 8 tokens): a page's box lands group by group, its parts side by side
+    } else if (!a.q4_pool) {  // (64 channels, 8 tokens, parts, groups of 8 tokens): a page's box lands group by group, its parts side by side
         uint64_t dims[4] = {64, 8, d / 64, pool_rows / 8};
         uint64_t strides[3] = {2 * d, 128, 16 * d};
         uint32_t box[4] = {64, 8, (uint32_t)d / 64, (uint32_t)a.g.bs / 8};
@@ -1036,8 +1295,9 @@ specpv_status launch_attention_tc(const AttnArgs& a, cudaStream_t stream) {
     p.part_ml = reinterpret_cast<float*>(ws + skip + (size_t)n_units * p.n_splits * p.R_pad * a.g.d * sizeof(float));
 
     const int n_lb = a.n_layers * a.batch;
-    if (a.g.d == 64) return launch_kernels<64, true>(p, n_lb, stream);
-    return 128 % G == 0 ? launch_kernels<128, false>(p, n_lb, stream) : launch_kernels<128, true>(p, n_lb, stream);
+    if (a.q4_pool) return a.g.d == 64 ? launch_kernels<64, false, true>(p, n_lb, stream) : launch_kernels<128, false, true>(p, n_lb, stream);
+    if (a.g.d == 64) return launch_kernels<64, true, false>(p, n_lb, stream);
+    return 128 % G == 0 ? launch_kernels<128, false, false>(p, n_lb, stream) : launch_kernels<128, true, false>(p, n_lb, stream);
 }
 
 }  // namespace specpv

@@ -18,6 +18,9 @@ struct TcParams {
     CUtensorMap tm_vnew;
     CUtensorMap tm_kpool;  // (64, 8, d/64, rows/8)    box (64, 8, d/64, page size / 8)  (pair kernel: (d, rows), box (64, page size))
     CUtensorMap tm_vpool;
+    const void* q4_pool;   // a cache in 4 bits: its pool, and the step's own keys and values
+    const void* k_new;
+    const void* v_new;
     const uint64_t* tree_mask;
     const int32_t* q_lens;
     const int32_t* block_table;
