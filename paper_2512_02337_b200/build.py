@@ -14,7 +14,7 @@ CSRC = PKG / "csrc"
 LIB = PKG / "lib" / "libspecpv.so"
 PYCALLS = PKG / "lib" / ("pycalls" + sysconfig.get_config_var("EXT_SUFFIX"))  # per interpreter: another one builds its own
 SOURCES = ["api.cu", "aux_kernels.cu", "attn_simt.cu", "attn_tc.cu", "attn_pair.cu", "score_tc.cu", "proj_tc.cu", "offload.cu",
-           "cache_q4.cu", "evict.cu", "selftest.cu"]
+           "cache_q4.cu", "attn_q4_rows.cu", "evict.cu", "selftest.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC,-fvisibility=hidden",

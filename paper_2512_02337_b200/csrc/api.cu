@@ -636,6 +636,7 @@ SPECPV_EXPORT specpv_status specpv_verify_full_q4(const specpv_config* cfg, int 
     a.partial_off = w.partial_off;
     a.partial_bytes = w.partial_bytes;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    if (attention_q4_rows_wanted(a)) return launch_attention_q4_rows(a, s);
     return attention_tc_supported(a) ? launch_attention_tc(a, s) : launch_attention_simt(a, s);
 }
 

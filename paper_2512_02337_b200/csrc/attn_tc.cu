@@ -237,6 +237,7 @@ __device__ __forceinline__ void open_tiles(const TcParams& p, const Job& c, Barr
     using Sh = Shape<D, true>;
     constexpr int kVTok = D / 8;  // tokens of a V tile per thread
     const int lane = tid & 31;
+    const uint32_t mask = p.q4_mask, ones = p.q4_ones;
     const uint32_t ring = c.q_smem + Sh::kQBytes, codes = ring + Sh::kStages * Sh::kSlotBytes, params = codes + Sh::kCodeStages * Sh::kCodeBytes;
     const int ppt = kTileTokens / p.bs;
     const int cg = tid % (D / 8), t0 = kV ? tid / (D / 8) * kVTok : tid;  // first token
@@ -326,8 +327,8 @@ __device__ __forceinline__ void open_tiles(const TcParams& p, const Job& c, Barr
                 const uint32_t to = row + (x >> 1) * 1024 + (((x & 1) << 6) ^ high);
 #pragma unroll
                 for (int y = 0; y < 4; ++y)
-                    store16(to + ((y << 4) ^ low), q4::fma_bf16x2(q4::open_pair(w[y], 0), scale, offset), q4::fma_bf16x2(q4::open_pair(w[y], 1), scale, offset),
-                            q4::fma_bf16x2(q4::open_pair(w[y], 2), scale, offset), q4::fma_bf16x2(q4::open_pair(w[y], 3), scale, offset));
+                    store16(to + ((y << 4) ^ low), q4::fma_bf16x2(q4::open_pair(w[y], 0, mask, ones), scale, offset), q4::fma_bf16x2(q4::open_pair(w[y], 1, mask, ones), scale, offset),
+                            q4::fma_bf16x2(q4::open_pair(w[y], 2, mask, ones), scale, offset), q4::fma_bf16x2(q4::open_pair(w[y], 3, mask, ones), scale, offset));
             }
         } else {
             const int left = is_page(entry) ? c.seq_len - (c.tile_begin + j) * kTileTokens - t0 : 0;  // valid tokens of the thread's
@@ -363,7 +364,7 @@ __device__ __forceinline__ void open_tiles(const TcParams& p, const Job& c, Barr
                         uint32_t even[4], odd[4];
 #pragma unroll
                         for (int y = 0; y < 4; ++y) {  // channels 2 y and 2 y + 1 of the eight
-                            const uint32_t a = q4::fma_bf16x2(q4::open_pair(w[2 * y], u), sc[u], of[u]), z = q4::fma_bf16x2(q4::open_pair(w[2 * y + 1], u), sc[u], of[u]);
+                            const uint32_t a = q4::fma_bf16x2(q4::open_pair(w[2 * y], u, mask, ones), sc[u], of[u]), z = q4::fma_bf16x2(q4::open_pair(w[2 * y + 1], u, mask, ones), sc[u], of[u]);
                             even[y] = __byte_perm(a, z, 0x5410);
                             odd[y] = __byte_perm(a, z, 0x7632);
                         }
@@ -1208,7 +1209,7 @@ specpv_status launch_attention_tc(const AttnArgs& a, cudaStream_t stream) {
         uint32_t box[4] = {64, (uint32_t)G, (uint32_t)(128 / G), 1};
         if (!encode_map(&p.tm_q, a.q, 4, dims, strides, box)) return SPECPV_ERR_CUDA;
     }
-    p.q4_pool = a.q4_pool; p.k_new = a.k_new; p.v_new = a.v_new;
+    p.q4_pool = a.q4_pool; p.k_new = a.k_new; p.v_new = a.v_new; p.q4_mask = q4::kMask; p.q4_ones = q4::kOnes;
     if (!a.q4_pool) {
         uint64_t dims[3] = {d, (uint64_t)Hkv, step_tokens};
         uint64_t strides[2] = {2 * d, (uint64_t)Hkv * 2 * d};

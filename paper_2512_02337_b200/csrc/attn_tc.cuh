@@ -21,6 +21,7 @@ struct TcParams {
     const void* q4_pool;   // a cache in 4 bits: its pool, and the step's own keys and values
     const void* k_new;
     const void* v_new;
+    uint32_t q4_mask, q4_ones;  // q4::kMask, q4::kOnes
     const uint64_t* tree_mask;
     const int32_t* q_lens;
     const int32_t* block_table;

@@ -162,6 +162,8 @@ struct AttnArgs {
 specpv_status launch_attention_simt(const AttnArgs& a, cudaStream_t stream);
 specpv_status launch_attention_tc(const AttnArgs& a, cudaStream_t stream);  // bf16
 bool attention_tc_supported(const AttnArgs& a);
+specpv_status launch_attention_q4_rows(const AttnArgs& a, cudaStream_t stream);  // bf16, a cache in 4 bits, few rows
+bool attention_q4_rows_wanted(const AttnArgs& a);
 // log-sum-exp merge of partial results [lb][Hkv][splits][M_max * G] (rows of d floats; natural-log maximum and sum) into out and lse
 specpv_status launch_merge_splits(const AttnArgs& a, int n_splits, float* part_o, float* part_ml, cudaStream_t stream);
 

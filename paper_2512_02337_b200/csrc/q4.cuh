@@ -29,6 +29,16 @@ __device__ __forceinline__ uint32_t open_pair(uint32_t w, int i) {
     const uint32_t x = i == 0 ? w : i == 1 ? w >> 4 : i == 2 ? w >> 8 : __funnelshift_r(w, w, 12);
     return (x & 0x00780078u) | 0x41804180u;
 }
+// The same where it is what a kernel does most: with both constants in registers (or the kernel's parameters) one instruction takes
+// the bits and puts them in place; of two immediates it could hold only one.  `mask` and `ones` are kMask and kOnes, as the compiler must
+// not know.
+constexpr uint32_t kMask = 0x00780078u, kOnes = 0x41804180u;
+__device__ __forceinline__ uint32_t open_pair(uint32_t w, int i, uint32_t mask, uint32_t ones) {
+    const uint32_t x = i == 0 ? w : i == 1 ? w >> 4 : i == 2 ? w >> 8 : __funnelshift_r(w, w, 12);
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "r"(mask), "r"(ones));  // (x & mask) | ones
+    return r;
+}
 __device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
     uint32_t r;
     asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
