@@ -1,5 +1,5 @@
 // Attention over a cache in 4 bits (layout: q4.cuh) for few query rows per KV head: a decoded token, a short draft.  bfloat16 steps,
-// head_dim 64 or 128, up to 64 rows.
+// head_dim 64 or 128, up to 16 rows.
 //
 // With few rows the cache's bytes are what the call takes, and the codes have to be opened at the rate of the memory: 128 tokens of a
 // KV head arrive every 0.4 us per SM.  Here they go from shared memory to registers and stay there: opened codes ARE the fragments of
@@ -14,7 +14,8 @@
 // eight: A's row 2 i + e of S^T is token 8 i + 2 s + e, which is where P^T, transposed in registers, needs it.
 //
 // A warp walks chunks of 64 tokens on its own (one to four pages, copied in bulk into stages of its own), with its own running maximum,
-// sums and accumulators; the warps of a CTA meet at the end, KV splits in the merge kernel.
+// sums and accumulators.  The CTAs, one per SM, take equal shares of all sequences' chunks, whatever their lengths; a share can end one
+// sequence's KV head and begin the next.  The warps of a CTA meet at the end of each, the CTAs in the merge kernel.
 // Precision: weights rounded to bfloat16 for the second product (2^-8 of each at most), their sums taken before that in float32.
 #include <type_traits>
 
@@ -28,21 +29,22 @@ namespace {
 using namespace tc;
 
 constexpr int kChunk = 64;               // tokens
-constexpr int kMaxRows = 64;             // of a KV head; also bounds the step's tokens, which are one chunk
+// Rows of a KV head; also bounds the step's tokens, which are one chunk.  (us, 65536 tokens x 8 layers, 4 / 8 / 16 rows of 128 here 145 / 146 /
+// 241, on the tcgen05 kernel 457 / 483 / 485; 32 rows in one CTA 552, as two CTAs of 16 459, there 486; 4096 tokens x 1 layer 43 / 26, there 16.)
+constexpr int kMaxRows = 16;
 constexpr float kRaise = 60.f;           // log2 of the weight from which references are raised
 
-// rows of a CTA: 8 NT.  More accumulators, fewer warps.
+// rows of a CTA: 8 NT
 template <int D, int NT>
 struct RowsShape {
-    static constexpr int kWarps = NT <= 2 ? 12 : 8;
-    static constexpr int kStages = 2;
+    static constexpr int kWarps = NT == 1 ? 12 : 8;
+    static constexpr int kStages = 2;  // per warp
     static constexpr int kStageBytes = kChunk * (D + 8);
     static constexpr int kPitch = D + 4;  // of the accumulators when the warps meet
     static constexpr int kRing = kWarps * kStages * kStageBytes;
     static constexpr int kMeet = kWarps * 8 * NT * kPitch * 4;
-    static constexpr int kStepV = D * kChunk * 2;
-    static constexpr int kQ = NT > 2 ? 8 * NT * D * 2 : 0;
-    static constexpr int kSmemBytes = (kRing > kMeet ? kRing : kMeet) + kStepV + kQ;
+    static constexpr int kStepV = D * kMaxRows * 2;
+    static constexpr int kSmemBytes = (kRing > kMeet ? kRing : kMeet) + kStepV;
 };
 
 struct RowsParams {
@@ -56,11 +58,11 @@ struct RowsParams {
     const int32_t* seq_lens;
     void* out;
     float* lse;
-    float* part_o;   // [lb][Hkv][splits][R_max][d]
-    float* part_ml;  // [lb][Hkv][splits][R_max][2], natural logarithm
+    float* part_o;   // [lb][Hkv][slots][R_max][d]
+    float* part_ml;  // [lb][Hkv][slots][R_max][2], natural logarithm
     void* workspace;
     int layer0, batch, M_max, mask_words, Hq, Hkv, G, bs, bs_log2, max_blocks, n_pages;
-    int n_splits, n_row_groups, out_f32;
+    int n_layers, n_slots;
     float scale_log2;
     uint32_t q4_mask, q4_ones;  // q4::kMask, q4::kOnes
 };
@@ -96,39 +98,79 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
     using S = RowsShape<D, NT>;
     constexpr int kWarps = S::kWarps, kThreads = 32 * kWarps, kRows = 8 * NT;
     constexpr int kWords = D / 32;        // of codes per lane and key
-    constexpr bool kQInSmem = NT > 2;
+    constexpr int kTogether = NT == 1 ? 4 : 2;  // steps of 16 tokens whose scores are worked on side by side
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ uint64_t full[kWarps][S::kStages];
     __shared__ uint32_t bad_pages[kWarps][S::kStages];
     __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows], s_factor[kWarps][kRows], s_sum[kRows], s_top[kRows];
     __shared__ int abort_flag, odd;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    int x = blockIdx.x;
-    const int rg = x % p.n_row_groups;
-    x /= p.n_row_groups;
-    const int split = x % p.n_splits;
-    x /= p.n_splits;
-    const int h = x % p.Hkv, lb = x / p.Hkv, b = lb % p.batch, l = lb / p.batch;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kWarps * S::kStages; ++i) mbar_init(smem_u32(&full[0][0] + i), 1);
         abort_flag = 0;
         odd = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    const uint32_t base = smem_u32(smem), step_v = base + (S::kRing > S::kMeet ? S::kRing : S::kMeet), q_smem = step_v + S::kStepV;
+    const uint32_t base = smem_u32(smem), step_v = base + (S::kRing > S::kMeet ? S::kRing : S::kMeet);
     __syncthreads();
-    if (p.n_splits == 1) pdl_trigger();
     pdl_wait();
+
+    // ---- the CTA's share: an equal part of the positions (chunks, and the step's tokens behind them) of all units, which are
+    // (layer, sequence, KV head) in that order.  At least so many positions that no unit meets more CTAs than it has slots.
+    auto positions_of = [&](int b) {
+        return b < p.batch ? (int)((min((long long)max(p.seq_lens[b], 0), (long long)p.max_blocks * p.bs) + kChunk - 1) / kChunk) + 1 : 0;
+    };
+    int per_head = 0, longest = 0;  // positions of a layer's KV head, all sequences
+    for (int b0 = 0; b0 < p.batch; b0 += 32) {
+        const int n = positions_of(b0 + lane);
+        per_head += __reduce_add_sync(0xffffffffu, n);
+        longest = max(longest, __reduce_max_sync(0xffffffffu, n));
+    }
+    const int total = per_head * p.Hkv * p.n_layers, least = (longest + p.n_slots - 2) / (p.n_slots - 1);
+    const int n_ctas = max(1, min((int)gridDim.x, total / max(least, 1)));
+    if ((int)blockIdx.x >= n_ctas) return;
+    // floor(total c / n_ctas) and its inverse (the last CTA whose share starts at or before a position); the quotients are no nearer
+    // than 1 / n_ctas to an integer that they are not, so that their floors are exact
+    auto share_at = [&](int c) { return (int)((double)total * c / n_ctas); };
+    auto cta_of = [&](int at) { return (int)(((double)(at + 1) * n_ctas - 1.0) / total); };
+    int at = share_at(blockIdx.x);
+    const int share_end = share_at(blockIdx.x + 1);
+    uint32_t fills = 0;  // chunks that the warp has taken from its stages so far
+    while (at < share_end) {
+    // ---- the unit at `at`, and the part of it that is the CTA's ----
+    const int l = at / (per_head * p.Hkv);
+    int in_layer = at - l * per_head * p.Hkv, b = 0, n_positions = 0;
+    for (int b0 = 0; n_positions == 0; b0 += 32) {  // (ends: in_layer lies within one of the sequences)
+        const int n = positions_of(b0 + lane);
+        int upto = n;  // inclusive sums over the lanes
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const unsigned beyond = __ballot_sync(0xffffffffu, upto * p.Hkv > in_layer);
+        const int found = beyond ? __ffs(beyond) - 1 : 31;
+        const int before = __shfl_sync(0xffffffffu, upto - n, found);
+        if (beyond) {
+            in_layer -= before * p.Hkv;
+            b = b0 + found;
+            n_positions = __shfl_sync(0xffffffffu, n, found);
+        } else {
+            in_layer -= __shfl_sync(0xffffffffu, upto, 31) * p.Hkv;
+            if (b0 + 32 >= p.batch) return;
+        }
+    }
+    const int h = in_layer / n_positions, begin = in_layer % n_positions, lb = l * p.batch + b;
+    const int n_chunks = min(n_positions - begin, share_end - at);
+    const int unit_at = at - begin;
+    const int first_cta = cta_of(unit_at), n_parts = cta_of(unit_at + n_positions - 1) - first_cta + 1, part = (int)blockIdx.x - first_cta;
+    at += n_chunks;
 
     const int seq_len = (int)min((long long)max(p.seq_lens[b], 0), (long long)p.max_blocks * p.bs);
     const int M = min(max(p.q_lens ? p.q_lens[b] : p.M_max, 0), p.M_max);
-    const int row0 = rg * kRows, rows = min(kRows, M * p.G - row0);
-    if (rows <= 0) return;  // (uniform for the CTA)
-    // KV range of this split: an equal share of the chunks and of the step's tokens, which come last
-    const int ctx_chunks = (seq_len + kChunk - 1) / kChunk;
-    const long long positions = ctx_chunks + 1;
-    const int begin = (int)(positions * split / p.n_splits), n_chunks = (int)(positions * (split + 1) / p.n_splits) - begin;
-    const bool last = split == p.n_splits - 1;
+    const int rows = M * p.G;
+    if (rows <= 0) continue;  // (uniform for the CTA)
+    const bool last = begin + n_chunks == n_positions;  // the step's tokens are here
     const int n_ctx = n_chunks - (last ? 1 : 0);
 
     // ---- copies: chunk i of the warp's (the CTA's chunk warp + i kWarps) into stage i % kStages ----
@@ -141,57 +183,50 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
         const int c = warp + i * kWarps, blk = (begin + c) * ppc + lane;
         return lane >= ppc || c >= n_ctx || (long long)blk * p.bs >= seq_len || blk >= p.max_blocks ? -1 : table[blk];
     };
+    const uint32_t fills0 = fills;
     auto copy = [&](int i, int page) {
         const int c = warp + i * kWarps, blk = (begin + c) * ppc + lane;
         if (c >= n_ctx) return;
         const bool wanted = lane < ppc && (long long)blk * p.bs < seq_len && blk < p.max_blocks, there = wanted && page >= 0 && page < p.n_pages;
         if (wanted && !there) record_fault(p.workspace, SPECPV_ERR_BAD_BLOCK_TABLE, b, blk, page, l);
         const uint32_t bad = __ballot_sync(0xffffffffu, wanted && !there), n = (uint32_t)__popc(__ballot_sync(0xffffffffu, there));
-        const uint32_t bar = smem_u32(&full[warp][i & 1]);
+        const uint32_t slot = (fills0 + i) % S::kStages, bar = smem_u32(&full[warp][slot]);
         if (lane == 0) {
-            bad_pages[warp][i & 1] = bad;
+            bad_pages[warp][slot] = bad;
             mbar_expect_tx(bar, n * page_bytes);
         }
         __syncwarp();
         if (there)
             asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                         ::"r"(ring + (i & 1) * S::kStageBytes + lane * page_bytes), "l"(pool + (size_t)page * p.Hkv * page_bytes), "r"(page_bytes), "r"(bar)
+                         ::"r"(ring + slot * S::kStageBytes + lane * page_bytes), "l"(pool + (size_t)page * p.Hkv * page_bytes), "r"(page_bytes), "r"(bar)
                          : "memory");
         __syncwarp();
     };
-    static_assert(S::kStages == 2, "stage = chunk & 1");
-    copy(0, entry_of(0));
-    copy(1, entry_of(1));
-    int next_entry = entry_of(2);
+    constexpr int kStages = S::kStages;
+    static_assert(kStages == 1 || kStages == 2, "stage = chunk % kStages");
+#pragma unroll
+    for (int i = 0; i < kStages; ++i) copy(i, entry_of(i));
+    int next_entry = entry_of(kStages);
 
     // ---- the rows' queries as B fragments; the step's values, transposed, in shared memory ----
-    uint32_t qf[kQInSmem ? 1 : NT][kQInSmem ? 1 : D / 8];
-    auto q_row = [&](int r) {
-        const int row = row0 + r;
-        return reinterpret_cast<const __nv_bfloat16*>(p.q) + (((size_t)lb * p.M_max + row / p.G) * p.Hq + h * p.G + row % p.G) * D;
-    };
-    if constexpr (kQInSmem) {  // [row][lane t][D / 8 words], words of a lane 16 bytes at a time, spread over the banks
-        for (int i = threadIdx.x; i < kRows * (D / 8); i += kThreads) {
-            const int r = i / (D / 8), piece = i % (D / 8);
+    uint32_t qf[NT][D / 8];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int r = n * 8 + g;
+        const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.q) +
+                                                          (((size_t)lb * p.M_max + r / p.G) * p.Hq + h * p.G + r % p.G) * D) + t * (D / 32);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
             uint4 v = make_uint4(0, 0, 0, 0);
-            if (r < rows) v = reinterpret_cast<const uint4*>(q_row(r))[piece];
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_smem + r * D * 2 + ((piece ^ (r & 7)) << 4)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+            if (r < rows) v = src[i];
+            qf[n][4 * i] = v.x; qf[n][4 * i + 1] = v.y; qf[n][4 * i + 2] = v.z; qf[n][4 * i + 3] = v.w;
         }
-    } else {
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (n * 8 + g < rows) v = reinterpret_cast<const uint4*>(q_row(n * 8 + g))[t * (D / 32) + i];
-                qf[n][4 * i] = v.x; qf[n][4 * i + 1] = v.y; qf[n][4 * i + 2] = v.z; qf[n][4 * i + 3] = v.w;
-            }
     }
     if (last) {
         const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(p.v_new) + ((size_t)lb * p.M_max * p.Hkv + h) * D;
-        uint16_t* dst = reinterpret_cast<uint16_t*>(smem + (step_v - base));  // [channel][64 tokens], 16-byte pieces swizzled by channel
+        uint16_t* dst = reinterpret_cast<uint16_t*>(smem + (step_v - base));  // [token / 8][channel][8 tokens]
         bool found = false;
-        for (int i = threadIdx.x; i < kChunk * D; i += kThreads) {
+        for (int i = threadIdx.x; i < kMaxRows * D; i += kThreads) {
             const int a = i / D, c = i % D;
             uint16_t v = 0;
             if (a < M) {
@@ -201,11 +236,11 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
                     v = 0;
                 }
             }
-            dst[c * kChunk + (((a >> 3) ^ (c & 7)) << 3) + (a & 7)] = v;
+            dst[((a >> 3) * D + c) * 8 + (a & 7)] = v;
         }
         if (found) odd = 1;
+        __syncthreads();
     }
-    if (kQInSmem || last) __syncthreads();
 
     // ---- where the lane's codes are in a stage (chunks of a page: keys [d / 32][bs][16 bytes], values [bs / 16][d][8 bytes]) ----
     const int bs_mask = p.bs - 1;
@@ -217,7 +252,7 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
         const uint32_t kp = (uint32_t)(kt >> p.bs_log2) * page_bytes, vp = (uint32_t)(vt >> p.bs_log2) * page_bytes;
         const int ka = kt & bs_mask, va = vt & bs_mask;
         k_off[i] = kp + (D == 128 ? (uint32_t)(t * p.bs + ka) * 16 : (uint32_t)((t >> 1) * p.bs + ka) * 16 + (t & 1) * 8);
-        k_par[i] = kp + (uint32_t)q4::param_at(p.bs, D, 0, ka) * 2;
+        k_par[i] = kp + (uint32_t)q4::param_at(p.bs, D, 0, ka & ~7) * 2;  // of the group of eight
         v_off[i] = vp + (uint32_t)q4::v_word(p.bs, D, va, g) * 4;
         v_par[i] = vp + (uint32_t)q4::param_at(p.bs, D, 2, va) * 2;
     }
@@ -237,19 +272,46 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
     auto work = [&](auto is_step, int i) {
         constexpr bool step = decltype(is_step)::value;
         const int chunk = warp + i * kWarps;
-        const uint32_t stage = ring + (i & 1) * S::kStageBytes;
+        const uint32_t slot = (fills0 + i) % kStages, stage = ring + slot * S::kStageBytes;
         const int left = step ? M : seq_len - (begin + chunk) * kChunk;  // valid tokens of the chunk, if fewer than 64
-        uint32_t bad = 0;
-        if (!step) {
-            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&full[warp][i & 1]), (i >> 1) & 1, &abort_flag, p.workspace, 41))) return false;
-            bad = bad_pages[warp][i & 1];
+        uint32_t bad;
+        if constexpr (!step) {
+            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&full[warp][slot]), (fills0 + i) / kStages & 1, &abort_flag, p.workspace, 41))) return false;
+            bad = bad_pages[warp][slot];
+            if (bad || left < kChunk) {
+                // Tokens behind a bad page id have no scales and offsets, nor (values) have those past the end: zeros.
+                for (int a = lane; a < kChunk; a += 32) {
+                    const int page = a >> p.bs_log2, at = a & (p.bs - 1);
+                    const bool gone = bad >> page & 1;
+                    uint16_t* par = reinterpret_cast<uint16_t*>(smem + (stage - base) + page * page_bytes);
+                    if (gone) par[q4::param_at(p.bs, D, 0, at)] = par[q4::param_at(p.bs, D, 1, at)] = 0;
+                    if (gone || a >= left) par[q4::param_at(p.bs, D, 2, at)] = par[q4::param_at(p.bs, D, 3, at)] = 0;
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before the stage is filled again
+                __syncwarp();
+            }
         }
         // ---- S^T and the weights, 16 tokens a step ----
         uint32_t pf[4][NT][2];
         float add[NT][2];
-        // A row's reference is its largest score in the warp's first chunk, which is looked at once for that before it is worked on.  It
-        // is raised when a weight passes 2^60 (float32 sums and bfloat16 weights keep their relative precision at any exponent).
+        uint32_t k_scale[2][4], k_offset[2][4];  // of tokens 2 s and 2 s + 1 of the lane's eight
+        const uint32_t half = g & 1 ? 0x3232 : 0x1010;
+        if constexpr (!step) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const uint4 a = lds16(stage + k_par[r]), z = lds16(stage + k_par[r] + two_bs);
+                k_scale[r][0] = a.x; k_scale[r][1] = a.y; k_scale[r][2] = a.z; k_scale[r][3] = a.w;
+                k_offset[r][0] = z.x; k_offset[r][1] = z.y; k_offset[r][2] = z.z; k_offset[r][3] = z.w;
+            }
+        }
+        // A row's reference is its largest score in the warp's first chunk (looked at once more where its scores are not all in
+        // registers together).  It is raised when a weight passes 2^60 (float32 sums and bfloat16 weights keep their relative precision at any exponent).
         bool look = i == 0;
+        auto reference = [&](float most) {
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+            return most == -INFINITY ? 0.f : most;  // (nothing seen)
+        };
         for (bool again = true; again;) {
             again = false;
             float most[NT][2];
@@ -259,8 +321,11 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
                 most[n][0] = most[n][1] = -INFINITY;
             }
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                float c[NT][4];
+            for (int s0 = 0; s0 < 4; s0 += kTogether) {
+            float cs[kTogether][NT][4];
+#pragma unroll
+            for (int s = s0; s < s0 + kTogether; ++s) {
+                float (&c)[NT][4] = cs[s - s0];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) c[n][0] = c[n][1] = c[n][2] = c[n][3] = 0.f;
                 uint32_t k[2][D / 8];  // pairs of channels of rows g and g + 8
@@ -275,10 +340,7 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
                             const uint2 v = lds8(stage + k_off[r] + s * 32);
                             w[0] = v.x; w[1] = v.y;
                         }
-                        uint32_t sc, of;
-                        asm volatile("{\n\t.reg .b16 x, y;\n\tld.shared.b16 x, [%2];\n\tld.shared.b16 y, [%3];\n\tmov.b32 %0, {x, x};\n\tmov.b32 %1, {y, y};\n\t}"
-                                     : "=r"(sc), "=r"(of) : "r"(stage + k_par[r] + s * 4), "r"(stage + k_par[r] + two_bs + s * 4) : "memory");
-                        if (bad >> ((k_token + 32 * r) >> p.bs_log2) & 1) sc = of = 0;
+                        const uint32_t sc = __byte_perm(k_scale[r][s], 0, half), of = __byte_perm(k_offset[r][s], 0, half);
 #pragma unroll
                         for (int i2 = 0; i2 < kWords; ++i2)
 #pragma unroll
@@ -298,22 +360,13 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
                     }
                 }
 #pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
+                for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        uint32_t b0, b1;
-                        if constexpr (kQInSmem) {
-                            const int piece = t * kWords + ks / 2;
-                            const uint2 v = lds8(q_smem + (n * 8 + g) * D * 2 + ((piece ^ g) << 4) + (ks & 1) * 8);
-                            b0 = v.x; b1 = v.y;
-                        } else {
-                            b0 = qf[n][2 * ks]; b1 = qf[n][2 * ks + 1];
-                        }
-                        mma_16816(c[n], k[0][2 * ks], k[1][2 * ks], k[0][2 * ks + 1], k[1][2 * ks + 1], b0, b1);
-                    }
-                }
+                    for (int n = 0; n < NT; ++n)
+                        mma_16816(c[n], k[0][2 * ks], k[1][2 * ks], k[0][2 * ks + 1], k[1][2 * ks + 1], qf[n][2 * ks], qf[n][2 * ks + 1]);
                 // tokens that are not there, or not seen: -infinity
                 if (step || left < kChunk) {
+                    asm volatile("" ::: "memory");  // a branch
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
                         const int a = k_token + 32 * r + 2 * s;
@@ -323,69 +376,89 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
                             for (int e = 0; e < 2; ++e) {
                                 bool seen = a < left;
                                 if (step) {
-                                    const int row = row0 + n * 8 + 2 * t + e;
-                                    seen = seen && row < row0 + rows && (p.tree_mask[((size_t)b * p.M_max + row / p.G) * p.mask_words] >> a & 1);
+                                    const int row = n * 8 + 2 * t + e;
+                                    seen = seen && row < rows && (p.tree_mask[((size_t)b * p.M_max + row / p.G) * p.mask_words] >> a & 1);
                                 }
                                 if (!seen) c[n][2 * r + e] = -INFINITY;
                             }
                     }
                 }
-                float top = -INFINITY;
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int s = 0; s < kTogether; ++s)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        c[n][e] = fmaf(c[n][e], scale, -m[n][e & 1]);
-                        top = fmaxf(top, c[n][e]);
+                        cs[s][n][e] = fmaf(cs[s][n][e], scale, -m[n][e & 1]);
+                        top = fmaxf(top, cs[s][n][e]);
                     }
-                if (look) {
+            if (look) {
+#pragma unroll
+                for (int s = 0; s < kTogether; ++s)
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) most[n][e & 1] = fmaxf(most[n][e & 1], c[n][e]);
+                        for (int e = 0; e < 4; ++e) most[n][e & 1] = fmaxf(most[n][e & 1], cs[s][n][e]);
+                if constexpr (kTogether < 4) {
                     continue;
-                }
-                if (__any_sync(0xffffffffu, top > kRaise)) {
-                    // references rise to the largest of these tokens; sums and accumulators follow, and the chunk starts over
+                } else {  // the whole chunk is here: no second pass
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            float rise = fmaxf(fmaxf(c[n][e], c[n][e + 2]), 0.f);
+                            m[n][e] = reference(most[n][e]);
 #pragma unroll
-                            for (int o = 4; o < 32; o <<= 1) rise = fmaxf(rise, __shfl_xor_sync(0xffffffffu, rise, o));
-                            const float factor = ex2(-rise);
-                            m[n][e] += rise;
-                            sum[n][e] *= factor;
-#pragma unroll
-                            for (int d = 0; d < D / 16; ++d) {
-                                acc[d][n][e] *= factor;
-                                acc[d][n][e + 2] *= factor;
+                            for (int s = 0; s < kTogether; ++s) {
+                                cs[s][n][e] -= m[n][e];
+                                cs[s][n][e + 2] -= m[n][e];
                             }
                         }
-                    again = true;
-                    break;
+                    look = false;
                 }
+            } else if (__any_sync(0xffffffffu, top > kRaise)) {
+                // references rise to the largest of these tokens; sums and accumulators follow, and the chunk starts over
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float rise = 0.f;
+#pragma unroll
+                        for (int s = 0; s < kTogether; ++s) rise = fmaxf(rise, fmaxf(cs[s][n][e], cs[s][n][e + 2]));
+#pragma unroll
+                        for (int o = 4; o < 32; o <<= 1) rise = fmaxf(rise, __shfl_xor_sync(0xffffffffu, rise, o));
+                        const float factor = ex2(-rise);
+                        m[n][e] += rise;
+                        sum[n][e] *= factor;
+#pragma unroll
+                        for (int d = 0; d < D / 16; ++d) {
+                            acc[d][n][e] *= factor;
+                            acc[d][n][e + 2] *= factor;
+                        }
+                    }
+                again = true;
+                break;
+            }
+#pragma unroll
+            for (int s = 0; s < kTogether; ++s)
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
+                    float (&c)[4] = cs[s][n];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        c[n][e] = ex2(c[n][e]);
-                        add[n][e & 1] += c[n][e];
+                        c[e] = ex2(c[e]);
+                        add[n][e & 1] += c[e];
                     }
-                    pf[s][n][0] = transposed(pack_bf16(c[n][0], c[n][1]));
-                    pf[s][n][1] = transposed(pack_bf16(c[n][2], c[n][3]));
+                    pf[s0 + s][n][0] = transposed(pack_bf16(c[0], c[1]));
+                    pf[s0 + s][n][1] = transposed(pack_bf16(c[2], c[3]));
                 }
             }
             if (look) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                        for (int o = 4; o < 32; o <<= 1) most[n][e] = fmaxf(most[n][e], __shfl_xor_sync(0xffffffffu, most[n][e], o));
-                        m[n][e] = most[n][e] == -INFINITY ? 0.f : most[n][e];
-                    }
+                    for (int e = 0; e < 2; ++e) m[n][e] = reference(most[n][e]);
                 look = false;
                 again = true;
             }
@@ -404,19 +477,6 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
                 sc[i2][0] = a.x; sc[i2][1] = a.y; sc[i2][2] = a.z; sc[i2][3] = a.w;
                 of[i2][0] = z.x; of[i2][1] = z.y; of[i2][2] = z.z; of[i2][3] = z.w;
             }
-            if (left < kChunk || bad) {  // a token that is not there: no scale, no offset, no value
-#pragma unroll
-                for (int i2 = 0; i2 < 2; ++i2) {
-                    const bool gone = bad >> ((8 * t + 32 * i2) >> p.bs_log2) & 1;
-#pragma unroll
-                    for (int s = 0; s < 4; ++s) {
-                        const int n = gone ? 0 : left - (8 * t + 32 * i2 + 2 * s);
-                        const uint32_t keep = n > 1 ? ~0u : n > 0 ? 0xFFFFu : 0u;
-                        sc[i2][s] &= keep;
-                        of[i2][s] &= keep;
-                    }
-                }
-            }
         }
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) {
@@ -431,8 +491,8 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int ch = 16 * d + g + 8 * (j & 1);
-                    const uint4 v = lds16(step_v + ch * (kChunk * 2) + (((t + 4 * (j >> 1)) ^ (ch & 7)) << 4));
+                    uint4 v = make_uint4(0, 0, 0, 0);  // (tokens 8 t .. of the first 32; there are at most 16)
+                    if (j < 2 && t < 2) v = lds16(step_v + (t * D + 16 * d + g + 8 * j) * 16);
                     a[j][0] = v.x; a[j][1] = v.y; a[j][2] = v.z; a[j][3] = v.w;
                 }
             }
@@ -443,8 +503,8 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
         }
         __syncwarp();
         if (!step) {
-            copy(i + 2, next_entry);
-            next_entry = entry_of(i + 3);
+            copy(i + kStages, next_entry);
+            next_entry = entry_of(i + kStages + 1);
         }
         return true;
     };
@@ -452,6 +512,7 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
     bool ok = true;
 #pragma unroll 1
     for (; ok && warp + i * kWarps < n_ctx; ++i) ok = work(std::false_type(), i);
+    fills = fills0 + i;
     if (ok && warp + i * kWarps < n_chunks) work(std::true_type(), i);
 
     // ---- the warps meet ----
@@ -497,7 +558,7 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
         }
     __syncthreads();
     for (int i = threadIdx.x; i < rows * D; i += kThreads) {
-        const int r = i / D, c = i % D, row = row0 + r, j = row / p.G, head = row % p.G;
+        const int r = i / D, c = i % D, j = r / p.G;
         float o = 0.f;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) o += meet[(w * kRows + r) * S::kPitch + c];
@@ -510,22 +571,29 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
                 if (!isfinite(y) && (seen >> a & 1)) o += y;
             }
         }
-        if (p.n_splits == 1) {
-            const size_t at = (((size_t)lb * p.M_max + j) * p.Hq + h * p.G + head) * D + c;
-            const float y = total == 0.f ? o : o / total;  // a row that has seen nothing is zero
-            if (p.out_f32) reinterpret_cast<float*>(p.out)[at] = y;
-            else reinterpret_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(y);
-            if (p.lse && c == 0) p.lse[at / D] = total == 0.f ? -INFINITY : fmaf(s_top[r], kLn2, logf(total));
-        } else {
-            const size_t at = (((size_t)lb * p.Hkv + h) * p.n_splits + split) * ((size_t)p.M_max * p.G) + row;
-            p.part_o[at * D + c] = o;
-            if (c == 0) {
-                // nothing seen: -infinity; a NaN has to survive the merge, which leaves out what weighs nothing
-                p.part_ml[at * 2] = total == 0.f ? -INFINITY : total != total ? INFINITY : s_top[r] * kLn2;
-                p.part_ml[at * 2 + 1] = total;
-            }
+        const size_t to = (((size_t)lb * p.Hkv + h) * p.n_slots + part) * ((size_t)p.M_max * p.G) + r;
+        p.part_o[to * D + c] = o;
+        if (c == 0) {
+            // nothing seen: -infinity; a NaN has to survive the merge, which leaves out what weighs nothing
+            p.part_ml[to * 2] = total == 0.f ? -INFINITY : total != total ? INFINITY : s_top[r] * kLn2;
+            p.part_ml[to * 2 + 1] = total;
         }
     }
+    if (last)  // slots that no CTA fills
+        for (int i = threadIdx.x; i < (p.n_slots - n_parts) * rows; i += kThreads) {
+            const size_t to = (((size_t)lb * p.Hkv + h) * p.n_slots + n_parts + i / rows) * ((size_t)p.M_max * p.G) + i % rows;
+            p.part_ml[to * 2] = -INFINITY;
+            p.part_ml[to * 2 + 1] = 0.f;
+        }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before copies into where the warps met
+    __syncthreads();
+    if (last) {
+        if (threadIdx.x == 0) odd = 0;
+        __syncthreads();
+    }
+    if (abort_flag) break;
+    }
+    pdl_trigger();
     if (abort_flag) __nanosleep(1000000);  // after a wait that gave up, the copies in flight land within microseconds
 }
 
@@ -550,41 +618,40 @@ specpv_status launch_attention_q4_rows(const AttnArgs& a, cudaStream_t stream) {
     p.block_table = a.block_table; p.seq_lens = a.seq_lens; p.out = a.out; p.lse = a.lse; p.workspace = a.workspace;
     p.layer0 = a.layer0; p.batch = a.batch; p.M_max = a.M_max; p.mask_words = a.mask_words; p.Hq = a.g.Hq; p.Hkv = a.g.Hkv; p.G = a.g.G;
     p.bs = a.g.bs; p.bs_log2 = a.g.bs == 16 ? 4 : a.g.bs == 32 ? 5 : 6;
-    p.max_blocks = a.max_blocks; p.n_pages = a.n_pages; p.out_f32 = a.g.out_f32;
+    p.max_blocks = a.max_blocks; p.n_pages = a.n_pages; p.n_layers = a.n_layers;
     p.scale_log2 = a.g.scale * kLog2e;
     p.q4_mask = q4::kMask; p.q4_ones = q4::kOnes;
     const int R_max = a.M_max * a.g.G, units = a.g.Hkv * a.n_layers * a.batch;
-    const int nt = R_max <= 8 ? 1 : R_max <= 16 ? 2 : 4;
-    p.n_row_groups = (R_max + 8 * nt - 1) / (8 * nt);
-    // KV splits by a cost model in microseconds, one CTA per SM: set-up, the rounds of its warps over their chunks, the meeting, and, with
-    // splits, the partial results' round trip and the merge
-    const int positions = (a.max_seq_len + kChunk - 1) / kChunk + 1, warps = nt <= 2 ? 12 : 8;
-    const long long base = (long long)units * p.n_row_groups;
-    const double round = nt == 1 ? 2.2 : nt == 2 ? 2.8 : 3.0;
-    const double row_bytes = (double)units * R_max * (a.g.d + 2) * sizeof(float);
-    double best = 1e300;
-    p.n_splits = 1;
-    for (int s = 1; s <= 64 && s <= positions; ++s) {
-        if (s > 1 && row_bytes * s > (double)a.partial_bytes) break;
-        const long long waves = (base * s + 147) / 148;
-        const int chunks = (positions + s - 1) / s;
-        double cost = waves * (5.0 + round * ((chunks + warps - 1) / warps));
-        if (s > 1) cost += 3.0 + row_bytes * s * 2.0 / 5.3e6;
-        if (cost < best) {
-            best = cost;
-            p.n_splits = s;
-        }
+    const int positions = (a.max_seq_len + kChunk - 1) / kChunk + 1;
+    if ((long long)units * positions >= 1LL << 30) return SPECPV_ERR_CAPACITY;
+    // One CTA per SM, each with at least a chunk for every warp.  Where the units are alike a number of CTAs that the units divide
+    // makes shares that lie in one unit each; else every SM has the same to do, but a unit more or two to begin and end, 4 us each.
+    // (A position takes some 0.29 us, 0.45 with 16 rows.)
+    const int warps = R_max <= 8 ? 12 : 8;
+    const double us = R_max <= 8 ? 0.29 : 0.45, begin_us = 4.0;
+    const int most = (positions + warps - 1) / warps;  // CTAs of a unit
+    long long n_ctas = (long long)units * most < 148 ? (long long)units * most : 148;
+    if (a.batch == 1 && units <= 148) {
+        const int k = 148 / units < most ? 148 / units : most;
+        const double together = (double)units * positions / n_ctas * us + begin_us * (2.0 + (double)units / n_ctas), apart = (double)positions / k * us + begin_us;
+        if (apart <= together) n_ctas = (long long)units * k;
     }
+    const long long all = (long long)units * positions;
+    const size_t slot_bytes = (size_t)units * R_max * (a.g.d + 2) * sizeof(float);
+    const long long share = all / n_ctas > 1 ? all / n_ctas : 1;
+    long long slots = (positions + share - 1) / share + 1;
+    if (a.batch > 1) slots = slots * 2;  // shorter sequences leave more CTAs to a longer one
+    if (slots > 64) slots = 64;
+    if (slots > (long long)(a.partial_bytes / slot_bytes)) slots = (long long)(a.partial_bytes / slot_bytes);
+    if (slots < 2) return SPECPV_ERR_CAPACITY;
+    p.n_slots = (int)slots;
     char* ws = reinterpret_cast<char*>(a.workspace) + a.partial_off;
     p.part_o = reinterpret_cast<float*>(ws);
-    p.part_ml = reinterpret_cast<float*>(ws + (size_t)units * p.n_splits * R_max * a.g.d * sizeof(float));
-    const long long n_ctas = base * p.n_splits;
-    if (n_ctas > 0x7FFFFFFF) return SPECPV_ERR_CAPACITY;
-    const auto launch = a.g.d == 64 ? (nt == 1 ? launch_rows_form<64, 1> : nt == 2 ? launch_rows_form<64, 2> : launch_rows_form<64, 4>)
-                                    : (nt == 1 ? launch_rows_form<128, 1> : nt == 2 ? launch_rows_form<128, 2> : launch_rows_form<128, 4>);
+    p.part_ml = reinterpret_cast<float*>(ws + (size_t)units * slots * R_max * a.g.d * sizeof(float));
+    const bool one = R_max <= 8;
+    const auto launch = a.g.d == 64 ? (one ? launch_rows_form<64, 1> : launch_rows_form<64, 2>) : (one ? launch_rows_form<128, 1> : launch_rows_form<128, 2>);
     const specpv_status st = launch(p, (int)n_ctas, stream);
-    if (st != SPECPV_OK || p.n_splits == 1) return st;
-    return launch_merge_splits(a, p.n_splits, p.part_o, p.part_ml, stream);
+    return st != SPECPV_OK ? st : launch_merge_splits(a, p.n_slots, p.part_o, p.part_ml, stream);
 }
 
 }  // namespace specpv
