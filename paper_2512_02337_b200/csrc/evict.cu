@@ -11,103 +11,189 @@ namespace {
 
 // ---------------------------------------------------------------------------------------------
 // Account: acc[t] += sum over the accepted rows i and the query heads g of the KV head of exp(scale q_ig . k_t - lse_ig), for the
-// tokens t that row i sees.  The sum over rows is formed by one thread per token, in row order, so that the result is the same
-// at every run.  Plain form: a thread owns a token, eight query rows at a time wait in shared memory as float32 and are read as
-// broadcasts.  grid = (groups of 128 tokens, KV heads, layers x seqs).
+// tokens t that row i sees.  The keys are read once, at the rate of the memory (that is the bound), straight into the registers that
+// the warp-wide matrix instruction takes them from: a warp owns 16 tokens at a time, S^T [16 tokens x 8 rows] = K Q^T.  The sum over
+// channels may be taken in any order, so lane (g, t) keeps the 16 bytes at 16 (4 j + t) of tokens g and g + 8 as they come.  The
+// rows' queries wait in shared memory in the same order, 16 bytes a lane.  float32: both factors as two terms of 11 bits, three
+// products (m16n8k8), which leaves 2^-21 of a product.  A token's sum over the rows is formed in a fixed order: the same at every run.
 // ---------------------------------------------------------------------------------------------
-constexpr int kAccTokens = 128;
-constexpr int kAccRows = 8;
+constexpr int kAccWarps = 8;
+constexpr int kAccTokens = 16;      // of a warp at a time
+constexpr int kAccPassRows = 128;   // rows per launch; more rows take several
 
-__device__ __forceinline__ void widen4(const float* p, float4& v) { v = *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ void widen4(const __nv_bfloat16* p, float4& v) {
-    const uint2 w = *reinterpret_cast<const uint2*>(p);
-    v = make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u));
+__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_tf32(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// x as two terms of 11 bits; an infinity or NaN goes into the first alone
+__device__ __forceinline__ void two_terms(uint32_t x, uint32_t& hi, uint32_t& lo) {
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(__uint_as_float(x)));
+    const float rest = __uint_as_float(x) - __uint_as_float(hi);
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(lo) : "f"(rest));
+    if ((x & 0x7F800000u) == 0x7F800000u) {
+        hi = x;
+        lo = 0;
+    }
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kAccTokens) accumulate_simt_kernel(AccumulateParams p) {
+__global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulateParams p) {
     pdl_begin(p.pdl);
-    __shared__ __align__(16) float s_q[kAccRows][D];
-    __shared__ float s_lse[kAccRows];
-    __shared__ int s_end[kAccRows];  // tokens that the row sees; 0 for a row that adds nothing
+    constexpr int kPieces = D * (int)sizeof(T) / 64;  // 16-byte pieces of a token per lane
+    constexpr bool kF32 = sizeof(T) == 4;
+    extern __shared__ __align__(16) unsigned char acc_smem[];
     const int h = blockIdx.y, lb = blockIdx.z, b = lb % p.batch, l = lb / p.batch;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int seq_len = min(max(p.seq_lens[b], 0), p.max_blocks * p.bs);
     const int n = min(max(p.n_accepted[b], 0), p.A_max);
-    const int t = blockIdx.x * kAccTokens + threadIdx.x;
-    if (blockIdx.x * kAccTokens >= seq_len || n == 0) return;
-    int page = -1;
-    if (t < seq_len) {
-        page = p.block_table[(size_t)b * p.max_blocks + t / p.bs];
-        if (page < 0 || page >= p.n_pages) {
-            record_fault(p.workspace, SPECPV_ERR_BAD_BLOCK_TABLE, b, t / p.bs, page, l);
-            page = -1;
+    const int n_tiles = (seq_len + kAccTokens - 1) / kAccTokens;
+    const int tile0 = blockIdx.x * p.tiles_per_cta, tile1 = min(tile0 + p.tiles_per_cta, n_tiles);
+    const int rows = min(p.row1, n * p.G) - p.row0, row_tiles = (rows + 7) / 8;
+    if (tile0 >= tile1 || rows <= 0) return;
+    uint4* s_q = reinterpret_cast<uint4*>(acc_smem);  // [row tile][piece][lane]
+    float* s_lse = reinterpret_cast<float*>(s_q + row_tiles * kPieces * 32);  // [row], log2; +infinity adds nothing
+    int* s_end = reinterpret_cast<int*>(s_lse + row_tiles * 8);  // tokens that the row sees
+    for (int i = threadIdx.x; i < row_tiles * 8; i += 32 * kAccWarps) {
+        const int r = p.row0 + i, a = r / p.G;
+        float lse = INFINITY;
+        int row = -1;
+        if (i < rows) {
+            row = p.accepted ? p.accepted[(size_t)b * p.A_max + a] : a;
+            if (row < 0 || row >= p.M_max) {
+                if (h == 0 && blockIdx.x == 0 && r % p.G == 0) record_fault(p.workspace, SPECPV_ERR_INVALID_ARG, b, a, row, l);
+                row = -1;
+            } else {
+                lse = p.lse[((size_t)lb * p.M_max + row) * p.Hq + h * p.G + r % p.G] * 1.4426950408889634f;
+                if (lse == -INFINITY) lse = INFINITY;
+            }
         }
+        s_lse[i] = lse;
+        s_end[i] = seq_len - n + a + 1;
+        const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.q) + (((size_t)lb * p.M_max + max(row, 0)) * p.Hq + h * p.G + r % p.G) * D);
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                s_q[((i >> 3) * kPieces + j) * 32 + (i & 7) * 4 + x] = row < 0 ? make_uint4(0, 0, 0, 0) : src[j * 4 + x];
     }
-    const T* k = reinterpret_cast<const T*>(p.k_pool) + ((((size_t)(p.layer0 + l) * p.n_pages + max(page, 0)) * p.Hkv + h) * p.bs + t % p.bs) * D;
-    float total = 0.f;
-    for (int r0 = 0; r0 < n * p.G; r0 += kAccRows) {
-        __syncthreads();  // the rows before have been read
-        for (int i = threadIdx.x; i < kAccRows * (D / 4); i += kAccTokens) {
-            const int r = r0 + i / (D / 4), c = i % (D / 4) * 4, a = r / p.G;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            float lse = 0.f;
-            int end = 0;
-            if (a < n) {
-                const int row = p.accepted ? p.accepted[(size_t)b * p.A_max + a] : a;
-                if (row >= 0 && row < p.M_max) {
-                    const size_t q = ((size_t)lb * p.M_max + row) * p.Hq + h * p.G + r % p.G;
-                    widen4(reinterpret_cast<const T*>(p.q) + q * D + c, v);
-                    lse = p.lse[q];
-                    end = lse == -INFINITY ? 0 : seq_len - n + a + 1;
-                } else if (c == 0 && h == 0 && blockIdx.x == 0 && r % p.G == 0) {
-                    record_fault(p.workspace, SPECPV_ERR_INVALID_ARG, b, a, row, l);
+    __syncthreads();
+    const uint4* k_pool = reinterpret_cast<const uint4*>(p.k_pool) + ((size_t)(p.layer0 + l) * p.n_pages * p.Hkv + h) * p.bs * (D * sizeof(T) / 16);
+    const size_t page_stride = (size_t)p.Hkv * p.bs * (D * sizeof(T) / 16);
+    const int32_t* table = p.block_table + (size_t)b * p.max_blocks;
+    float* acc = p.acc + (((size_t)(p.layer0 + l) * p.batch + b) * p.Hkv + h) * (size_t)p.max_blocks * p.bs;
+    const float scale = p.scale * 1.4426950408889634f;
+    auto entry_of = [&](int tile) { return tile < tile1 ? table[tile * kAccTokens / p.bs] : -1; };
+    uint4 next[2][kPieces];
+    bool next_ok = false;
+    auto fetch = [&](int tile, int page) {  // keys of tokens g and g + 8
+        next_ok = page >= 0 && page < p.n_pages;
+        if (tile >= tile1) return;
+        if (!next_ok) {
+            if (lane == 0) record_fault(p.workspace, SPECPV_ERR_BAD_BLOCK_TABLE, b, tile * kAccTokens / p.bs, page, l);
+            return;
+        }
+        const uint4* src = k_pool + page * page_stride + (size_t)(tile * kAccTokens % p.bs + g) * (D * sizeof(T) / 16) + t;
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) next[r][j] = src[r * 8 * (D * sizeof(T) / 16) + j * 4];
+    };
+    int tile = tile0 + warp;
+    int entry = entry_of(tile + kAccWarps);
+    fetch(tile, entry_of(tile));
+    for (; tile < tile1; tile += kAccWarps) {
+        uint32_t k[2][kPieces * 4];
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                k[r][4 * j] = next[r][j].x; k[r][4 * j + 1] = next[r][j].y; k[r][4 * j + 2] = next[r][j].z; k[r][4 * j + 3] = next[r][j].w;
+            }
+        const bool ok = next_ok;
+        const int token = tile * kAccTokens + g;
+        float* mine = acc + token + 8 * t;  // of lanes t = 0 and 1
+        const bool writes = ok && t < 2 && token + 8 * t < seq_len;
+        const float before = writes ? *mine : 0.f;
+        fetch(tile + kAccWarps, entry);
+        entry = entry_of(tile + 2 * kAccWarps);
+        const bool all_seen = (tile + 1) * kAccTokens <= seq_len - n;
+        float sum[2] = {0.f, 0.f};
+#pragma unroll 1
+        for (int rt = 0; rt < row_tiles; ++rt) {
+            float c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                const uint4 q = s_q[(rt * kPieces + j) * 32 + lane];
+                if constexpr (!kF32) {
+                    mma_bf16(c, k[0][4 * j], k[1][4 * j], k[0][4 * j + 1], k[1][4 * j + 1], q.x, q.y);
+                    mma_bf16(c, k[0][4 * j + 2], k[1][4 * j + 2], k[0][4 * j + 3], k[1][4 * j + 3], q.z, q.w);
+                } else {
+                    const uint32_t qw[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                    for (int x = 0; x < 4; x += 2) {
+                        uint32_t ah[4], al[4], bh[2], bl[2];
+                        two_terms(k[0][4 * j + x], ah[0], al[0]);
+                        two_terms(k[1][4 * j + x], ah[1], al[1]);
+                        two_terms(k[0][4 * j + x + 1], ah[2], al[2]);
+                        two_terms(k[1][4 * j + x + 1], ah[3], al[3]);
+                        two_terms(qw[x], bh[0], bl[0]);
+                        two_terms(qw[x + 1], bh[1], bl[1]);
+                        mma_tf32(c, al[0], al[1], al[2], al[3], bh[0], bh[1]);
+                        mma_tf32(c, ah[0], ah[1], ah[2], ah[3], bl[0], bl[1]);
+                        mma_tf32(c, ah[0], ah[1], ah[2], ah[3], bh[0], bh[1]);
+                    }
                 }
             }
-            *reinterpret_cast<float4*>(&s_q[i / (D / 4)][c]) = v;
-            if (c == 0) {
-                s_lse[i / (D / 4)] = lse;
-                s_end[i / (D / 4)] = end;
+            const float2 lse = *reinterpret_cast<const float2*>(s_lse + rt * 8 + 2 * t);
+            float w[4] = {tc::ex2(fmaf(c[0], scale, -lse.x)), tc::ex2(fmaf(c[1], scale, -lse.y)), tc::ex2(fmaf(c[2], scale, -lse.x)),
+                          tc::ex2(fmaf(c[3], scale, -lse.y))};
+            if (!all_seen) {
+                const int2 end = *reinterpret_cast<const int2*>(s_end + rt * 8 + 2 * t);
+                if (token >= end.x) w[0] = 0.f;
+                if (token >= end.y) w[1] = 0.f;
+                if (token + 8 >= end.x) w[2] = 0.f;
+                if (token + 8 >= end.y) w[3] = 0.f;
             }
-        }
-        __syncthreads();
-        if (page < 0) continue;
-        float4 sum[kAccRows];
-#pragma unroll
-        for (int j = 0; j < kAccRows; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int c = 0; c < D; c += 4) {
-            float4 x;
-            widen4(k + c, x);
-#pragma unroll
-            for (int j = 0; j < kAccRows; ++j) {
-                const float4 q = *reinterpret_cast<const float4*>(&s_q[j][c]);
-                sum[j].x = fmaf(q.x, x.x, sum[j].x);
-                sum[j].y = fmaf(q.y, x.y, sum[j].y);
-                sum[j].z = fmaf(q.z, x.z, sum[j].z);
-                sum[j].w = fmaf(q.w, x.w, sum[j].w);
-            }
+            sum[0] += w[0] + w[1];
+            sum[1] += w[2] + w[3];
         }
 #pragma unroll
-        for (int j = 0; j < kAccRows; ++j)
-            if (t < s_end[j]) total += expf(((sum[j].x + sum[j].y) + (sum[j].z + sum[j].w)) * p.scale - s_lse[j]);
+        for (int o = 1; o < 4; o <<= 1) {
+            sum[0] += __shfl_xor_sync(0xffffffffu, sum[0], o);
+            sum[1] += __shfl_xor_sync(0xffffffffu, sum[1], o);
+        }
+        if (writes) *mine = before + (t ? sum[1] : sum[0]);
     }
-    if (page >= 0) p.acc[(((size_t)(p.layer0 + l) * p.batch + b) * p.Hkv + h) * (size_t)p.max_blocks * p.bs + t] += total;
 }
 
 // ---------------------------------------------------------------------------------------------
-// Close-up: rank j of a KV head's kept tokens (ascending, so idx[j] >= j) moves to place j, in place.  A unit is the keys or the values
-// of one (layer, sequence, KV head); it is worked through in chunks of ranks, each read whole before any of it is written: place j, as
-// a source, belongs to a rank <= j, so nothing that is still to be read is overwritten, and later chunks may be read ahead.  Ranks
-// that stay (a prefix) are skipped.  grid = (2 KV heads, layers x seqs).
+// Close-up: rank j of a KV head's kept tokens (ascending, so idx[j] >= j) moves to place j, in place.  A unit is the keys, the values or
+// the accounts of one (layer, sequence, KV head).  Keys and values are worked through in rounds of ranks, by a cluster of CTAs side by
+// side: a round is read whole before any of it is written (a cluster barrier between), and then nothing is overwritten that is still to
+// be read, because place j, as a source, belongs to a rank <= j.  For the same reason the next round's rows are read, and the
+// indexes and table entries of the one after that, before this round's are written.  Ranks that stay (a prefix) are skipped.  Bound by
+// memory: every moved row is read and written once.  grid = (cluster x 3 KV heads, layers x seqs).
 // ---------------------------------------------------------------------------------------------
 constexpr int kCloseThreads = 256;
-constexpr int kCloseLoads = 8;  // 16-byte loads in flight per thread
+constexpr int kCloseLoads = 8;  // 16-byte loads in flight per thread and round
+constexpr int kAccLoads = 16;   // accounts per thread and round
+constexpr uint32_t kNoRow = 0xFFFFFFFFu;
 
-__global__ void __launch_bounds__(kCloseThreads) close_up_kernel(EvictParams p) {
-    pdl_begin(p.pdl);
-    const int h = blockIdx.x % p.Hkv, values = blockIdx.x / p.Hkv, lb = blockIdx.y, b = lb % p.batch, l = lb / p.batch;
+__global__ void __launch_bounds__(kCloseThreads, 2) close_up_kernel(EvictParams p) {
+    asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
+    uint32_t rank, n_ctas;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n_ctas));
+    const int unit = blockIdx.x / n_ctas, h = unit % p.Hkv, kind = unit / p.Hkv;  // 0 keys, 1 values, 2 accounts
+    const int lb = blockIdx.y, b = lb % p.batch, l = lb / p.batch;
     const int capacity = p.max_blocks * p.bs, seq_len = min(max(p.seq_lens[b], 0), capacity);
-    if (seq_len <= p.keep) return;
+    if (seq_len <= p.keep) return;  // (the whole cluster)
     const int32_t* idx = p.idx + (((size_t)l * p.batch + b) * p.Hkv + h) * p.keep;
     const int32_t* table = p.block_table + (size_t)b * p.max_blocks;
     // the first rank that moves
@@ -117,47 +203,80 @@ __global__ void __launch_bounds__(kCloseThreads) close_up_kernel(EvictParams p) 
         if (idx[mid] == mid) first = lo = mid + 1;
         else hi = mid;
     }
-    uint4* pool = reinterpret_cast<uint4*>(values ? p.v_pool : p.k_pool);
-    const int chunks = p.row_bytes / 16, per_chunk = kCloseThreads * kCloseLoads / chunks;  // 16-byte pieces of a row, ranks at a time
-    const int piece = threadIdx.x % chunks, lane_row = threadIdx.x / chunks, step = kCloseThreads / chunks;
-    auto place = [&](int t) -> long long {  // of token t, in 16-byte pieces; -1 behind a bad page id
-        const int page = table[t / p.bs];
-        if (page < 0 || page >= p.n_pages) {
-            if (piece == 0) record_fault(p.workspace, SPECPV_ERR_BAD_BLOCK_TABLE, b, t / p.bs, page, l);
-            return -1;
-        }
-        return ((((long long)l * p.n_pages + page) * p.Hkv + h) * p.bs + t % p.bs) * chunks + piece;
-    };
-    for (int j0 = first; j0 < p.keep; j0 += per_chunk) {
-        uint4 buf[kCloseLoads];
-        long long to[kCloseLoads];
+    if (kind == 2) {
+        if (rank) return;  // (no cluster barrier on this path)
+        float* acc = p.acc + (((size_t)l * p.batch + b) * p.Hkv + h) * (size_t)capacity;
+        for (int j0 = first; j0 < p.keep; j0 += kCloseThreads * kAccLoads) {
+            float a[kAccLoads];
 #pragma unroll
-        for (int u = 0; u < kCloseLoads; ++u) {
-            const int j = j0 + u * step + lane_row;
-            to[u] = -1;
-            if (j < p.keep) {
-                const long long from = place(idx[j]);
-                if (from >= 0) {
-                    to[u] = place(j);
-                    buf[u] = pool[from];
-                }
+            for (int u = 0; u < kAccLoads; ++u) {
+                const int j = j0 + u * kCloseThreads + threadIdx.x;
+                a[u] = j < p.keep ? acc[idx[j]] : 0.f;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < kAccLoads; ++u) {
+                const int j = j0 + u * kCloseThreads + threadIdx.x;
+                if (j < p.keep) acc[j] = a[u];
             }
         }
         __syncthreads();
+        for (int j = p.keep + threadIdx.x; j < seq_len; j += kCloseThreads) acc[j] = 0.f;  // the accounts of the tokens to come
+        return;
+    }
+    uint4* pool = reinterpret_cast<uint4*>(kind ? p.v_pool : p.k_pool);
+    const int chunks = p.row_bytes / 16, step = kCloseThreads / chunks;  // 16-byte pieces of a row, rows side by side
+    const int piece = threadIdx.x % chunks, lane_row = threadIdx.x / chunks, per_cta = step * kCloseLoads, per_round = per_cta * (int)n_ctas;
+    const uint32_t row0 = ((uint32_t)l * p.n_pages * p.Hkv + h) * p.bs, page_rows = (uint32_t)p.Hkv * p.bs;
+    auto row_of = [&](int t) -> uint32_t {  // of token t in the pool; none behind a bad page id
+        const int page = table[t / p.bs];
+        if (page < 0 || page >= p.n_pages) {
+            if (piece == 0) record_fault(p.workspace, SPECPV_ERR_BAD_BLOCK_TABLE, b, t / p.bs, page, l);
+            return kNoRow;
+        }
+        return row0 + (uint32_t)page * page_rows + t % p.bs;
+    };
+    uint32_t from_next[kCloseLoads], to_next[kCloseLoads], to[kCloseLoads];
+    uint4 buf[2][kCloseLoads];
+    auto look_up = [&](int j0) {
+#pragma unroll
+        for (int u = 0; u < kCloseLoads; ++u) {
+            const int j = j0 + (int)rank * per_cta + u * step + lane_row;
+            from_next[u] = to_next[u] = kNoRow;
+            if (j < p.keep) {
+                from_next[u] = row_of(idx[j]);
+                to_next[u] = row_of(j);
+                if (to_next[u] == kNoRow) from_next[u] = kNoRow;
+                if (from_next[u] == kNoRow) to_next[u] = kNoRow;
+            }
+        }
+    };
+    auto load = [&](uint4 (&x)[kCloseLoads]) {
+#pragma unroll
+        for (int u = 0; u < kCloseLoads; ++u) {
+            to[u] = to_next[u];
+            if (from_next[u] != kNoRow) x[u] = pool[(size_t)from_next[u] * chunks + piece];
+        }
+    };
+    auto round = [&](int j0, uint4 (&now)[kCloseLoads], uint4 (&next)[kCloseLoads]) {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // this round's rows have been read
+        uint32_t dst[kCloseLoads];
+#pragma unroll
+        for (int u = 0; u < kCloseLoads; ++u) dst[u] = to[u];
+        load(next);
+        look_up(j0 + 2 * per_round);
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 #pragma unroll
         for (int u = 0; u < kCloseLoads; ++u)
-            if (to[u] >= 0) pool[to[u]] = buf[u];
+            if (dst[u] != kNoRow) pool[(size_t)dst[u] * chunks + piece] = now[u];
+    };
+    look_up(first);
+    load(buf[0]);
+    look_up(first + per_round);
+    for (int j0 = first; j0 < p.keep; j0 += 2 * per_round) {
+        round(j0, buf[0], buf[1]);
+        if (j0 + per_round < p.keep) round(j0 + per_round, buf[1], buf[0]);
     }
-    if (values) return;
-    float* acc = p.acc + (((size_t)l * p.batch + b) * p.Hkv + h) * (size_t)capacity;
-    for (int j0 = first; j0 < p.keep; j0 += kCloseThreads) {
-        const int j = j0 + threadIdx.x;
-        const float a = j < p.keep ? acc[idx[j]] : 0.f;
-        __syncthreads();
-        if (j < p.keep) acc[j] = a;
-    }
-    __syncthreads();
-    for (int j = p.keep + threadIdx.x; j < seq_len; j += kCloseThreads) acc[j] = 0.f;  // the accounts of the tokens to come
 }
 
 constexpr int kLensThreads = 128;
@@ -175,18 +294,51 @@ __global__ void __launch_bounds__(kLensThreads) evict_lens_kernel(EvictParams p)
         count_launch();                                                        \
     } while (0)
 
-specpv_status launch_accumulate(const AccumulateParams& p, int n_layers, int max_seq_len, int dtype, int d, cudaStream_t stream) {
-    if (max_seq_len <= 0) return SPECPV_OK;
-    const dim3 grid((max_seq_len + kAccTokens - 1) / kAccTokens, p.Hkv, n_layers * p.batch);
-    if (dtype == SPECPV_DTYPE_F32)
-        SPECPV_LAUNCH((d == 64 ? accumulate_simt_kernel<float, 64> : accumulate_simt_kernel<float, 128>), grid, kAccTokens, 0, stream, p);
-    else
-        SPECPV_LAUNCH((d == 64 ? accumulate_simt_kernel<__nv_bfloat16, 64> : accumulate_simt_kernel<__nv_bfloat16, 128>), grid, kAccTokens, 0, stream, p);
+template <typename T, int D>
+static specpv_status launch_accumulate_typed(AccumulateParams p, int n_layers, int max_seq_len, cudaStream_t stream) {
+    // A warp should have a few tiles to hide its start behind, the launch CTAs enough to fill the SMs twice
+    const long long tiles = (max_seq_len + kAccTokens - 1) / kAccTokens, heads = (long long)p.Hkv * n_layers * p.batch;
+    long long per_warp = tiles * heads / (kAccWarps * 4LL * 148);
+    per_warp = per_warp < 1 ? 1 : per_warp > 16 ? 16 : per_warp;
+    p.tiles_per_cta = (int)per_warp * kAccWarps;
+    const dim3 grid((unsigned)((tiles + p.tiles_per_cta - 1) / p.tiles_per_cta), p.Hkv, n_layers * p.batch);
+    const int all_rows = p.A_max * p.G;
+    for (p.row0 = 0; p.row0 < all_rows; p.row0 += kAccPassRows) {
+        p.row1 = p.row0 + kAccPassRows;
+        const int row_tiles = ((all_rows < p.row1 ? all_rows : p.row1) - p.row0 + 7) / 8;
+        const size_t smem = (size_t)row_tiles * 8 * (D * sizeof(T) + 8);
+        if (!tc::set_smem_limit_once(reinterpret_cast<const void*>(accumulate_kernel<T, D>), kAccPassRows * (D * (int)sizeof(T) + 8))) return SPECPV_ERR_CUDA;
+        SPECPV_LAUNCH((accumulate_kernel<T, D>), grid, 32 * kAccWarps, smem, stream, p);
+    }
     return SPECPV_OK;
 }
 
+specpv_status launch_accumulate(const AccumulateParams& p, int n_layers, int max_seq_len, int dtype, int d, cudaStream_t stream) {
+    if (max_seq_len <= 0) return SPECPV_OK;
+    if (dtype == SPECPV_DTYPE_F32)
+        return d == 64 ? launch_accumulate_typed<float, 64>(p, n_layers, max_seq_len, stream) : launch_accumulate_typed<float, 128>(p, n_layers, max_seq_len, stream);
+    return d == 64 ? launch_accumulate_typed<__nv_bfloat16, 64>(p, n_layers, max_seq_len, stream) : launch_accumulate_typed<__nv_bfloat16, 128>(p, n_layers, max_seq_len, stream);
+}
+
 specpv_status launch_evict(const EvictParams& p, int n_layers, cudaStream_t stream) {
-    SPECPV_LAUNCH(close_up_kernel, dim3(2 * p.Hkv, n_layers * p.batch), kCloseThreads, 0, stream, p);
+    // CTAs of a unit: enough to fill the SMs three times over
+    const long long units = 2LL * p.Hkv * n_layers * p.batch;
+    unsigned cluster = 1;
+    while (cluster < 8 && units * cluster < 3 * 148) cluster *= 2;
+    cudaLaunchAttribute attr[2]{};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(cluster * 3 * p.Hkv, n_layers * p.batch);
+    cfg.blockDim = kCloseThreads;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    if (cudaLaunchKernelEx(&cfg, close_up_kernel, p) != cudaSuccess) return SPECPV_ERR_CUDA;
+    count_launch();
     SPECPV_LAUNCH(evict_lens_kernel, dim3((p.batch + kLensThreads - 1) / kLensThreads), kLensThreads, 0, stream, p);
     return SPECPV_OK;
 }
