@@ -731,7 +731,7 @@ SPECPV_EXPORT specpv_status specpv_evict_tokens(const specpv_config* cfg, const 
     EvictParams p{};
     p.k_pool = kv->k_pool; p.v_pool = kv->v_pool; p.block_table = kv->block_table; p.seq_lens = const_cast<int32_t*>(kv->seq_lens);
     p.acc = acc; p.idx = idx; p.workspace = workspace;
-    p.batch = kv->batch; p.Hkv = g.Hkv; p.bs = g.bs; p.row_bytes = g.d * g.es; p.keep = keep_tokens; p.max_blocks = kv->max_blocks;
+    p.batch = kv->batch; p.Hkv = g.Hkv; p.bs = g.bs; p.row_bytes = g.d * g.es; p.keep = keep_tokens; p.sink = sink_tokens; p.max_blocks = kv->max_blocks;
     p.n_pages = kv->n_pages;
     return launch_evict(p, g.n_layers, s);
 }

@@ -132,7 +132,7 @@ struct EvictParams {
     float* acc;
     const int32_t* idx;  // kept tokens of every (layer, sequence, KV head), ascending
     void* workspace;
-    int batch, Hkv, bs, row_bytes, keep, max_blocks, n_pages;
+    int batch, Hkv, bs, row_bytes, keep, sink, max_blocks, n_pages;
     int pdl;  // set by launch_pdl_if
 };
 

@@ -176,9 +176,10 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
 // Close-up: rank j of a KV head's kept tokens (ascending, so idx[j] >= j) moves to place j, in place.  A unit is the keys, the values or
 // the accounts of one (layer, sequence, KV head).  Keys and values are worked through in rounds of ranks, by a cluster of CTAs side by
 // side: a round is read whole before any of it is written (a cluster barrier between), and then nothing is overwritten that is still to
-// be read, because place j, as a source, belongs to a rank <= j.  For the same reason the next round's rows are read, and the
-// indexes and table entries of the one after that, before this round's are written.  Ranks that stay (a prefix) are skipped.  Bound by
-// memory: every moved row is read and written once.  grid = (cluster x 3 KV heads, layers x seqs).
+// be read, because place j, as a source, belongs to a rank <= j.  For the same reason the next round's rows are requested before this
+// one's are written; where they are is known by then: one thread per row has asked for its index three rounds ahead and for the
+// table entries two ahead, so that no request waits for another.  Rows that stay are neither read nor written.  Bound by memory: every
+// moved row is read and written once.  grid = (cluster x 3 KV heads, layers x seqs).
 // ---------------------------------------------------------------------------------------------
 constexpr int kCloseThreads = 256;
 constexpr int kCloseLoads = 8;  // 16-byte loads in flight per thread and round
@@ -187,22 +188,17 @@ constexpr uint32_t kNoRow = 0xFFFFFFFFu;
 
 __global__ void __launch_bounds__(kCloseThreads, 2) close_up_kernel(EvictParams p) {
     asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
+    __shared__ uint2 s_rows[2][kCloseThreads];  // from, to; of the rounds of either parity
     uint32_t rank, n_ctas;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n_ctas));
     const int unit = blockIdx.x / n_ctas, h = unit % p.Hkv, kind = unit / p.Hkv;  // 0 keys, 1 values, 2 accounts
-    const int lb = blockIdx.y, b = lb % p.batch, l = lb / p.batch;
+    const int lb = blockIdx.y, b = lb % p.batch, l = lb / p.batch, tid = threadIdx.x;
     const int capacity = p.max_blocks * p.bs, seq_len = min(max(p.seq_lens[b], 0), capacity);
     if (seq_len <= p.keep) return;  // (the whole cluster)
     const int32_t* idx = p.idx + (((size_t)l * p.batch + b) * p.Hkv + h) * p.keep;
     const int32_t* table = p.block_table + (size_t)b * p.max_blocks;
-    // the first rank that moves
-    int first = 0;
-    for (int lo = 0, hi = p.keep; lo < hi;) {
-        const int mid = (lo + hi) / 2;
-        if (idx[mid] == mid) first = lo = mid + 1;
-        else hi = mid;
-    }
+    const int first = p.sink;  // the ranks before it stay
     if (kind == 2) {
         if (rank) return;  // (no cluster barrier on this path)
         float* acc = p.acc + (((size_t)l * p.batch + b) * p.Hkv + h) * (size_t)capacity;
@@ -210,72 +206,94 @@ __global__ void __launch_bounds__(kCloseThreads, 2) close_up_kernel(EvictParams 
             float a[kAccLoads];
 #pragma unroll
             for (int u = 0; u < kAccLoads; ++u) {
-                const int j = j0 + u * kCloseThreads + threadIdx.x;
+                const int j = j0 + u * kCloseThreads + tid;
                 a[u] = j < p.keep ? acc[idx[j]] : 0.f;
             }
             __syncthreads();
 #pragma unroll
             for (int u = 0; u < kAccLoads; ++u) {
-                const int j = j0 + u * kCloseThreads + threadIdx.x;
+                const int j = j0 + u * kCloseThreads + tid;
                 if (j < p.keep) acc[j] = a[u];
             }
         }
         __syncthreads();
-        for (int j = p.keep + threadIdx.x; j < seq_len; j += kCloseThreads) acc[j] = 0.f;  // the accounts of the tokens to come
+        for (int j = p.keep + tid; j < seq_len; j += kCloseThreads) acc[j] = 0.f;  // the accounts of the tokens to come
         return;
     }
     uint4* pool = reinterpret_cast<uint4*>(kind ? p.v_pool : p.k_pool);
     const int chunks = p.row_bytes / 16, step = kCloseThreads / chunks;  // 16-byte pieces of a row, rows side by side
-    const int piece = threadIdx.x % chunks, lane_row = threadIdx.x / chunks, per_cta = step * kCloseLoads, per_round = per_cta * (int)n_ctas;
+    const int piece = tid % chunks, lane_row = tid / chunks, per_cta = step * kCloseLoads, per_round = per_cta * (int)n_ctas;
     const uint32_t row0 = ((uint32_t)l * p.n_pages * p.Hkv + h) * p.bs, page_rows = (uint32_t)p.Hkv * p.bs;
-    auto row_of = [&](int t) -> uint32_t {  // of token t in the pool; none behind a bad page id
-        const int page = table[t / p.bs];
-        if (page < 0 || page >= p.n_pages) {
-            if (piece == 0) record_fault(p.workspace, SPECPV_ERR_BAD_BLOCK_TABLE, b, t / p.bs, page, l);
-            return kNoRow;
-        }
-        return row0 + (uint32_t)page * page_rows + t % p.bs;
+    // a thread's row of a round: rank j, -1 where there is none
+    auto rank_of = [&](int round) {
+        const int j = first + round * per_round + (int)rank * per_cta + tid;
+        return tid < per_cta && j < p.keep ? j : -1;
     };
-    uint32_t from_next[kCloseLoads], to_next[kCloseLoads], to[kCloseLoads];
+    auto index_of = [&](int round) {
+        const int j = rank_of(round);
+        return j >= 0 ? idx[j] : -1;
+    };
+    struct Pages { int from, to; };
+    auto pages_of = [&](int round, int token) {
+        const int j = rank_of(round);
+        Pages e{0, 0};
+        if (j >= 0) {
+            e.from = table[token / p.bs];
+            e.to = table[j / p.bs];
+        }
+        return e;
+    };
+    auto publish = [&](int round, int token, Pages e) {  // where the row goes from and to
+        const int j = rank_of(round);
+        uint2 r = make_uint2(kNoRow, kNoRow);
+        if (j >= 0 && j != token) {
+            const bool from_ok = e.from >= 0 && e.from < p.n_pages, to_ok = e.to >= 0 && e.to < p.n_pages;
+            if (from_ok && to_ok)
+                r = make_uint2(row0 + (uint32_t)e.from * page_rows + token % p.bs, row0 + (uint32_t)e.to * page_rows + j % p.bs);
+            else
+                record_fault(p.workspace, SPECPV_ERR_BAD_BLOCK_TABLE, b, (from_ok ? j : token) / p.bs, from_ok ? e.to : e.from, l);
+        }
+        s_rows[round & 1][tid] = r;
+    };
+    uint32_t to[kCloseLoads];
     uint4 buf[2][kCloseLoads];
-    auto look_up = [&](int j0) {
+    auto load = [&](int round, uint4 (&x)[kCloseLoads]) {
 #pragma unroll
         for (int u = 0; u < kCloseLoads; ++u) {
-            const int j = j0 + (int)rank * per_cta + u * step + lane_row;
-            from_next[u] = to_next[u] = kNoRow;
-            if (j < p.keep) {
-                from_next[u] = row_of(idx[j]);
-                to_next[u] = row_of(j);
-                if (to_next[u] == kNoRow) from_next[u] = kNoRow;
-                if (from_next[u] == kNoRow) to_next[u] = kNoRow;
-            }
+            const uint2 r = s_rows[round & 1][u * step + lane_row];
+            to[u] = r.y;
+            if (r.x != kNoRow) x[u] = pool[(size_t)r.x * chunks + piece];
         }
     };
-    auto load = [&](uint4 (&x)[kCloseLoads]) {
-#pragma unroll
-        for (int u = 0; u < kCloseLoads; ++u) {
-            to[u] = to_next[u];
-            if (from_next[u] != kNoRow) x[u] = pool[(size_t)from_next[u] * chunks + piece];
-        }
-    };
-    auto round = [&](int j0, uint4 (&now)[kCloseLoads], uint4 (&next)[kCloseLoads]) {
+    const int n_rounds = (p.keep - first + per_round - 1) / per_round;
+    // three rounds of look-ups under way
+    const int t0 = index_of(0), t1 = index_of(1);
+    int token2 = index_of(2), token3 = index_of(3);
+    const Pages e0 = pages_of(0, t0), e1 = pages_of(1, t1);
+    Pages pages2 = pages_of(2, token2);
+    publish(0, t0, e0);
+    publish(1, t1, e1);
+    __syncthreads();
+    load(0, buf[0]);
+    auto round = [&](int i, uint4 (&now)[kCloseLoads], uint4 (&next)[kCloseLoads]) {
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // this round's rows have been read
         uint32_t dst[kCloseLoads];
 #pragma unroll
         for (int u = 0; u < kCloseLoads; ++u) dst[u] = to[u];
-        load(next);
-        look_up(j0 + 2 * per_round);
+        load(i + 1, next);
+        publish(i + 2, token2, pages2);  // (the rows of round i have been taken from their place, by every thread: see the barrier below)
+        pages2 = pages_of(i + 3, token3);
+        token2 = token3;
+        token3 = index_of(i + 4);
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 #pragma unroll
         for (int u = 0; u < kCloseLoads; ++u)
             if (dst[u] != kNoRow) pool[(size_t)dst[u] * chunks + piece] = now[u];
+        __syncthreads();  // the rows of round i + 2 are there, those of round i + 1 taken
     };
-    look_up(first);
-    load(buf[0]);
-    look_up(first + per_round);
-    for (int j0 = first; j0 < p.keep; j0 += 2 * per_round) {
-        round(j0, buf[0], buf[1]);
-        if (j0 + per_round < p.keep) round(j0 + per_round, buf[1], buf[0]);
+    for (int i = 0; i < n_rounds; i += 2) {
+        round(i, buf[0], buf[1]);
+        if (i + 1 < n_rounds) round(i + 1, buf[1], buf[0]);
     }
 }
 
