@@ -62,14 +62,10 @@ __device__ __forceinline__ q4::Row quantise_row(const float (&x)[D / 32], uint32
         hi = fmaxf(hi, x[i]);
         finite &= isfinite(x[i]);
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    }
+    asm volatile("redux.sync.min.f32 %0, %1, 0xffffffff;" : "=f"(lo) : "f"(lo));
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(hi) : "f"(hi));
     const q4::Row r = q4::row_of(lo, hi, __all_sync(0xffffffffu, finite));
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) codes[i] = q4::code_of(r, x[i]);
+    q4::codes_of(r, x, codes);
     return r;
 }
 
@@ -100,18 +96,37 @@ __global__ void __launch_bounds__(kCommitThreads) commit_q4_kernel(CommitQ4Param
                           (((size_t)(p.layer0 + l) * p.n_pages + page) * p.Hkv + h) * q4::page_bytes(p.bs, D);
     uint32_t* words = reinterpret_cast<uint32_t*>(base);
     uint16_t* params = reinterpret_cast<uint16_t*>(base);
+    // the next token's rows are in flight while this one's are worked on
+    float k_next[C], v_next[C];
+    int row_next = -1;
+    auto fetch = [&](int t) {
+        if (t >= t1) return;
+        const int a = t - seq_len;
+        row_next = p.accepted ? p.accepted[(size_t)b * p.A_max + a] : a;
+        if (row_next < 0 || row_next >= p.M_max) return;
+        const size_t src = ((size_t)lb * p.M_max + row_next) * p.Hkv + h;
+        load_row<T, D>(p.k_new, src, lane, k_next);
+        load_row<T, D>(p.v_new, src, lane, v_next);
+    };
+    bool lost = false;
+    fetch(t0 + warp);
     for (int t = t0 + warp; t < t1; t += kCommitWarps) {
-        const int a = t - seq_len, row = p.accepted ? p.accepted[(size_t)b * p.A_max + a] : a, at = t - page_t0;
+        const int a = t - seq_len, row = row_next, at = t - page_t0;
+        float k[C], v[C];
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            k[i] = k_next[i];
+            v[i] = v_next[i];
+        }
+        fetch(t + kCommitWarps);
         if (row < 0 || row >= p.M_max) {  // the token keeps what its place held
             if (lane == 0) record_fault(p.workspace, SPECPV_ERR_INVALID_ARG, b, a, row, l);
 #pragma unroll
             for (int i = 0; i < C; ++i) s_v[at][lane * C + i] = 0xFF;
+            lost = true;
             continue;
         }
-        const size_t src = ((size_t)lb * p.M_max + row) * p.Hkv + h, out = ((size_t)lb * p.A_max + a) * p.Hkv + h;
-        float k[C], v[C];
-        load_row<T, D>(p.k_new, src, lane, k);
-        load_row<T, D>(p.v_new, src, lane, v);
+        const size_t out = ((size_t)lb * p.A_max + a) * p.Hkv + h;
         uint32_t kc[C], vc[C];
         const q4::Row kr = quantise_row<D>(k, kc), vr = quantise_row<D>(v, vc);
         store_values<T, D>(p.k_values, out, lane, kc, kr);
@@ -130,13 +145,14 @@ __global__ void __launch_bounds__(kCommitThreads) commit_q4_kernel(CommitQ4Param
             params[q4::param_at(p.bs, D, lane, at)] = x;
         }
     }
-    __syncthreads();
+    const bool skipped = __syncthreads_or(lost);
     // value words of the touched groups of eight tokens
     const int g0 = (t0 - page_t0) / 8, g1 = (t1 - 1 - page_t0) / 8;
     for (int i = threadIdx.x; i < (g1 - g0 + 1) * D; i += kCommitThreads) {
         const int g = g0 + i / D, c = i % D, at0 = g * 8;
         uint32_t* to = words + q4::v_word(p.bs, D, at0, c);
-        uint32_t w = q4::unrotated(*to);
+        const bool whole = page_t0 + at0 >= t0 && page_t0 + at0 + 8 <= t1 && !skipped;  // nothing of the old word stays
+        uint32_t w = whole ? 0u : q4::unrotated(*to);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int t = page_t0 + at0 + e;
@@ -241,14 +257,27 @@ __global__ void __launch_bounds__(kGatherThreads) gather_q4_kernel(GatherQ4Param
     const size_t out = (((size_t)l * p.part_pages + to) * p.Hkv + h) * p.bs * D;
     T* k = reinterpret_cast<T*>(p.part_k) + out;
     T* v = reinterpret_cast<T*>(p.part_v) + out;
-    for (int i = threadIdx.x; i < n_valid * (D / 8); i += kGatherThreads) {
-        const int t = i / (D / 8), c = i % (D / 8) * 8;
-        const uint32_t w = words[q4::k_word(p.bs, t, c)];
-        const uint32_t scale = q4::twice(params[q4::param_at(p.bs, D, 0, t)]), offset = q4::twice(params[q4::param_at(p.bs, D, 1, t)]);
-        uint32_t x[4];
+    constexpr int kBatch = 4;  // words in flight per thread
+    for (int i0 = threadIdx.x; i0 < n_valid * (D / 8); i0 += kBatch * kGatherThreads) {
+        uint32_t w[kBatch], scale[kBatch], offset[kBatch];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = q4::fma_bf16x2(q4::open_pair(w, e), scale, offset);
-        store8(k + (size_t)t * D + c, x);
+        for (int u = 0; u < kBatch; ++u) {
+            const int i = i0 + u * kGatherThreads, t = i / (D / 8), c = i % (D / 8) * 8;
+            if (t < n_valid) {
+                w[u] = words[q4::k_word(p.bs, t, c)];
+                scale[u] = params[q4::param_at(p.bs, D, 0, t)];
+                offset[u] = params[q4::param_at(p.bs, D, 1, t)];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int i = i0 + u * kGatherThreads, t = i / (D / 8), c = i % (D / 8) * 8;
+            if (t >= n_valid) break;
+            uint32_t x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = q4::fma_bf16x2(q4::open_pair(w[u], e), scale[u] * 0x10001u, offset[u] * 0x10001u);
+            store8(k + (size_t)t * D + c, x);
+        }
     }
     for (int i = threadIdx.x; i < p.bs / 16 * (D / 8); i += kGatherThreads) {
         const int t0 = i / (D / 8) * 16, c = i % (D / 8) * 8;
@@ -262,11 +291,18 @@ __global__ void __launch_bounds__(kGatherThreads) gather_q4_kernel(GatherQ4Param
             w[2 * j + 1][0] = x.z;
             w[2 * j + 1][1] = x.w;
         }
+        uint32_t scales[8], offsets[8];  // of pairs of tokens
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint4 x = *reinterpret_cast<const uint4*>(params + q4::param_at(p.bs, D, 2, t0 + 8 * j));
+            const uint4 y = *reinterpret_cast<const uint4*>(params + q4::param_at(p.bs, D, 3, t0 + 8 * j));
+            scales[4 * j] = x.x; scales[4 * j + 1] = x.y; scales[4 * j + 2] = x.z; scales[4 * j + 3] = x.w;
+            offsets[4 * j] = y.x; offsets[4 * j + 1] = y.y; offsets[4 * j + 2] = y.z; offsets[4 * j + 3] = y.w;
+        }
 #pragma unroll
         for (int pair = 0; pair < 8; ++pair) {  // tokens t0 + 2 pair and the next
             const int t = t0 + 2 * pair;
-            const uint32_t scale = *reinterpret_cast<const uint32_t*>(params + q4::param_at(p.bs, D, 2, t));
-            const uint32_t offset = *reinterpret_cast<const uint32_t*>(params + q4::param_at(p.bs, D, 3, t));
+            const uint32_t scale = scales[pair], offset = offsets[pair];
             uint32_t even[4], odd[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {

@@ -80,9 +80,26 @@ __device__ __forceinline__ Row row_of(float lo, float hi, bool finite) {
     }
     return r;
 }
-__device__ __forceinline__ uint32_t code_of(const Row& r, float x) {
-    const float n = rintf(__fdiv_rn(__fsub_rn(x, r.base), r.scale));  // 0 / 0, a row of equal elements: fmaxf takes the 0
-    return (uint32_t)fminf(fmaxf(n, 0.f), 15.f);
+// Codes of a lane's elements: the nearest integers of (x - base) / scale, ties to even, by IEEE division.  A multiplication by the
+// reciprocal is off by some 2^-23 of at most 16, so that it names another integer only next to a tie: where it comes that near (or the
+// reciprocal is not to be trusted) the warp divides after all.
+template <int N>
+__device__ __forceinline__ void codes_of(const Row& r, const float (&x)[N], uint32_t (&codes)[N]) {
+    const float inv = __frcp_rn(r.scale);
+    bool exact = !(r.scale > 1e-37f);  // (a row of equal elements, or one that is NaN, among them)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float q = fminf(fmaxf(__fsub_rn(x[i], r.base) * inv, 0.f), 15.f), m = q + 12582912.f;  // 1.5 2^23: rounds to an integer
+        exact |= fabsf(q - (m - 12582912.f)) > 0.4999f;
+        codes[i] = __float_as_uint(m) & 15u;
+    }
+    if (__any_sync(0xffffffffu, exact)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float n = rintf(__fdiv_rn(__fsub_rn(x[i], r.base), r.scale));
+            codes[i] = (uint32_t)fminf(fmaxf(n, 0.f), 15.f);  // 0 / 0: fmaxf takes the 0
+        }
+    }
 }
 
 }  // namespace q4
