@@ -33,6 +33,8 @@
 // cutting off the sums over the tokens), 5.4e-5 / 3.3e-8 / 3.4e-8, 1.79e-3 / 1.66e-3 / 1.66e-3 and 6.5e-4 / 4.5e-6 / 3.9e-7
 // (4101 tokens, 60 x 4 rows of 64).  It takes half again the contractions of P V and a third more of the softmax: 24.6 -> 31.4 us and
 // 16.1 -> 18.7 us for one layer, where the plain kernel took 1310 and 375.
+#include <type_traits>
+
 #include "attn_tc.cuh"
 #include "q4.cuh"
 
@@ -180,8 +182,11 @@ __device__ __forceinline__ void produce(const TcParams& p, const Job& c, Barrier
 }
 
 // =========================== a cache in 4 bits (kQ4) ======================================
-// The producer copies a tile's codes, two copies per page, and eight more warps open them to bfloat16 into the ring, where the tensor
-// maps would have delivered them.
+// The producer copies a tile's codes, two copies per page, and more warps open them to bfloat16 into the ring, where the tensor maps
+// would have delivered them.  With one row tile per CTA, four warps open the K tiles and four the V tiles: a K/V tile then costs them
+// less than its contractions.  With two row tiles, whose contractions take twice as long, four warps open both and the softmax keeps
+// 192 registers a thread instead of 168, with which it spills (64K tokens x 8 layers, 8 KV heads, four and eight warps: 8 rows x 4
+// 651 and 482 us, 60 rows x 4 603 and 690 us).
 template <int D>
 __device__ __forceinline__ void produce_codes(const TcParams& p, const Job& c, Barriers& bars, int lane) {
     using Sh = Shape<D, true>;
@@ -228,43 +233,44 @@ __device__ __forceinline__ void produce_codes(const TcParams& p, const Job& c, B
     }
 }
 
-// Four warps open the K tiles, four the V tiles (one warp per scheduler waits for its own results: with four for both, a tile took
-// 4200 cycles, its contractions 1350).  A thread owns a token of a K tile (16 bytes of codes of 32 channels at a time), and eight
-// channels of 16 (8 with 64 channels) tokens of a V tile, whose pairs of tokens become pairs of channels in registers.  V rows past
-// the valid tokens, and what is behind a bad page id, become zeros here.
-template <int D, bool kV>
+// 128 threads open the K tiles, the V tiles or both.  A thread owns a token of a K tile and a channel of a V tile: eight of its channels, or of its
+// tokens, are a word of codes and 16 bytes of the tile, whose rows are tokens (K) or channels (V: [2 x 64 tokens][D channels][64 tokens],
+// which the contraction takes as well as the other order; with rows of tokens, pairs of tokens had to become pairs of channels).  V
+// columns past the valid tokens, and what is behind a bad page id, become zeros.
+enum { kOpenK = 1, kOpenV = 2 };
+template <int D, int kDo>
 __device__ __forceinline__ void open_tiles(const TcParams& p, const Job& c, Barriers& bars, bool one, int tid) {
     using Sh = Shape<D, true>;
-    constexpr int kVTok = D / 8;  // tokens of a V tile per thread
     const int lane = tid & 31;
     const uint32_t mask = p.q4_mask, ones = p.q4_ones;
     const uint32_t ring = c.q_smem + Sh::kQBytes, codes = ring + Sh::kStages * Sh::kSlotBytes, params = codes + Sh::kCodeStages * Sh::kCodeBytes;
-    const int ppt = kTileTokens / p.bs;
-    const int cg = tid % (D / 8), t0 = kV ? tid / (D / 8) * kVTok : tid;  // first token
-    const int at_page = t0 % p.bs, page_in_tile = t0 / p.bs;
-    // within a stage: pages of bs D bytes of codes and 4 bs bytes of value scales and offsets
-    const uint32_t my_codes = codes + page_in_tile * p.bs * D + (kV ? q4::v_word(p.bs, D, at_page, cg * 8) * 4 : at_page * 16);
-    const uint32_t my_params = params + page_in_tile * p.bs * 4 + at_page * 2, two_bs = 2u * p.bs;
-    const char* k_params = reinterpret_cast<const char*>(p.q4_pool) + ((size_t)(p.layer0 + c.l) * p.n_pages * p.Hkv + c.h) * q4::page_bytes(p.bs, D) +
-                           q4::param_at(p.bs, D, 0, at_page) * 2;
-    const uint32_t page_stride = (uint32_t)(p.Hkv * q4::page_bytes(p.bs, D));
+    const int bs = p.bs, ppt = kTileTokens / bs;
+    const uint32_t two_bs = 2u * bs;
     const int32_t* table = p.block_table + (size_t)c.b * p.max_blocks;
-    auto entry_of = [&](int j) {  // of the thread's page of tile j
-        const int blk = (c.tile_begin + j) * ppt + page_in_tile;
-        return j >= c.n_ctx_tiles || (long long)blk * p.bs >= c.seq_len || blk >= p.max_blocks ? -1 : table[blk];
+    auto entry_of = [&](int j, int page) {  // of page `page` of tile j
+        const int blk = (c.tile_begin + j) * ppt + page;
+        return j >= c.n_ctx_tiles || (long long)blk * bs >= c.seq_len || blk >= p.max_blocks ? -1 : table[blk];
     };
     auto is_page = [&](int entry) { return entry >= 0 && entry < p.n_pages; };
-    // a key's scale and offset come straight from memory, a tile ahead
+    // K: the thread's token, its codes within a stage, its scale and offset straight from memory, a tile ahead
+    const int k_page = tid / bs, k_at = tid % bs;
+    const uint32_t k_codes = codes + k_page * bs * D + k_at * 16;
+    const char* k_params = reinterpret_cast<const char*>(p.q4_pool) + ((size_t)(p.layer0 + c.l) * p.n_pages * p.Hkv + c.h) * q4::page_bytes(bs, D) +
+                           q4::param_at(bs, D, 0, k_at) * 2;
+    const uint32_t page_stride = (uint32_t)(p.Hkv * q4::page_bytes(bs, D));
     uint32_t scale_next = 0, offset_next = 0;
     auto fetch_params = [&](int entry) {
         scale_next = offset_next = 0;
-        if (kV || !is_page(entry)) return;
+        if (!is_page(entry)) return;
         const char* base = k_params + (size_t)entry * page_stride;
         scale_next = *reinterpret_cast<const uint16_t*>(base);
         offset_next = *reinterpret_cast<const uint16_t*>(base + two_bs);
     };
-    int entry = entry_of(kV ? 0 : 1);  // V: of tile j; K: of tile j + 1
-    if (!kV) fetch_params(entry_of(0));
+    // V: the thread's channel; with 64 channels two threads share one, 64 tokens each
+    const int channel = tid % D, v_unit0 = tid / D * 4;
+    constexpr int kUnits = D / 16;  // of 16 tokens per thread
+    int v_entry = entry_of(0, min(lane, ppt - 1)), k_entry = entry_of(1, k_page);  // a lane per page of tile j; of tile j + 1
+    if (kDo & kOpenK) fetch_params(entry_of(0, k_page));
 
     auto store16 = [](uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
@@ -274,115 +280,105 @@ __device__ __forceinline__ void open_tiles(const TcParams& p, const Job& c, Barr
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
         return v;
     };
-    auto load4 = [](uint32_t at) {
-        uint32_t v;
-        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-        return v;
+    auto open = [&](uint32_t to, uint32_t w, const uint4& s, const uint4& o) {
+        store16(to, q4::fma_bf16x2(q4::open_pair(w, 0, mask, ones), s.x, o.x), q4::fma_bf16x2(q4::open_pair(w, 1, mask, ones), s.y, o.y),
+                q4::fma_bf16x2(q4::open_pair(w, 2, mask, ones), s.z, o.z), q4::fma_bf16x2(q4::open_pair(w, 3, mask, ones), s.w, o.w));
     };
-#pragma unroll 1
-    for (int j = 0; j < c.n_tiles; ++j) {
+    auto tile = [&](auto is_v, int j) {
+        constexpr bool kV = decltype(is_v)::value;
         const bool step = j >= c.n_ctx_tiles;
         const uint32_t stage = j & 1;
         // ring uses: K0 V0 K1 V1 .. with two row tiles, K0 K1 V0 K2 V1 K3 .. with one
         const int use = !one ? 2 * j + kV : kV ? (j < c.n_tiles - 1 ? 2 * j + 2 : 2 * j + 1) : max(2 * j - 1, 0);
         const uint32_t slot = (uint32_t)use % Sh::kStages, round = (uint32_t)use / Sh::kStages;
         bool ok = true;
-        if (!step) ok = mbar_wait(smem_u32(&bars.code_full[stage]), (j >> 1) & 1, &bars.abort_flag, p.workspace, 13);
+        if (!step && (!kV || kDo == kOpenV)) ok = mbar_wait(smem_u32(&bars.code_full[stage]), (j >> 1) & 1, &bars.abort_flag, p.workspace, 13);
         if (round) ok &= mbar_wait(smem_u32(&bars.kv_empty[slot]), (round + 1) & 1, &bars.abort_flag, p.workspace, 11);
-        if (!__all_sync(0xffffffffu, ok)) return;
+        if (!__all_sync(0xffffffffu, ok)) return false;
         const uint32_t dst = ring + slot * Sh::kSlotBytes;
-        if (step) {
-            // the step's own tokens, 16 bytes at a time, rows past them zero; values that are infinite or NaN go another way
-            const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(kV ? p.v_new : p.k_new) +
-                                                              ((size_t)c.lb * p.M_max * p.Hkv + c.h) * D);
-            bool found = false;
+        const uint32_t v_row = dst + channel * 128, v_swizzle = (channel & 7) << 4;
+        if (!kV && step) {  // the step's own keys, 16 bytes at a time, rows past them zero
+            const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.k_new) + ((size_t)c.lb * p.M_max * p.Hkv + c.h) * D);
 #pragma unroll 2
             for (int x = tid; x < kTileTokens * (D / 8); x += 128) {
                 const int t = x / (D / 8), chunk = x % (D / 8);
                 uint4 v = make_uint4(0, 0, 0, 0);
                 if (t < c.M) v = src[(size_t)t * p.Hkv * (D / 8) + chunk];
-                if (kV) {
-                    uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const bool lo = (w[y] & 0x7F80u) == 0x7F80u, hi = (w[y] & 0x7F800000u) == 0x7F800000u;
-                        found |= lo | hi;
-                        w[y] &= (lo ? 0xFFFF0000u : ~0u) & (hi ? 0xFFFFu : ~0u);
-                    }
-                    v = make_uint4(w[0], w[1], w[2], w[3]);
-                }
                 store16(dst + (t >> 3) * Sh::kGroupBytes + (chunk >> 3) * 1024 + (t & 7) * 128 + (((chunk & 7) ^ (t & 7)) << 4), v.x, v.y, v.z, v.w);
+            }
+        } else if (kV && step) {  // its values, eight tokens of the channel at a time; those that are infinite or NaN go another way
+            const uint16_t* src = reinterpret_cast<const uint16_t*>(p.v_new) + ((size_t)c.lb * p.M_max * p.Hkv + c.h) * D + channel;
+            bool found = false;
+#pragma unroll 1
+            for (int x = v_unit0 * 2; x < v_unit0 * 2 + kUnits * 2; ++x) {
+                uint32_t w[4];
+#pragma unroll
+                for (int y = 0; y < 8; ++y) {
+                    const int t = 8 * x + y;
+                    uint32_t v = t < c.M ? src[(size_t)t * p.Hkv * D] : 0u;
+                    if ((v & 0x7F80u) == 0x7F80u) {
+                        found = true;
+                        v = 0;
+                    }
+                    w[y / 2] = y & 1 ? w[y / 2] | v << 16 : v;
+                }
+                store16(v_row + (x >> 3) * (D * 128) + (((x & 7) << 4) ^ v_swizzle), w[0], w[1], w[2], w[3]);
             }
             if (found) bars.odd = 1;
         } else if (!kV) {
-            const uint32_t scale = scale_next * 0x10001u, offset = offset_next * 0x10001u;
-            fetch_params(entry);
-            entry = entry_of(j + 2);
-            const uint32_t at = my_codes + stage * Sh::kCodeBytes, row = dst + (tid >> 3) * Sh::kGroupBytes + (tid & 7) * 128;
+            const uint32_t s = scale_next * 0x10001u, o = offset_next * 0x10001u;
+            const uint4 scale = make_uint4(s, s, s, s), offset = make_uint4(o, o, o, o);
+            fetch_params(k_entry);
+            k_entry = entry_of(j + 2, k_page);
+            const uint32_t at = k_codes + stage * Sh::kCodeBytes, row = dst + (tid >> 3) * Sh::kGroupBytes + (tid & 7) * 128;
             const uint32_t low = (tid & 3) << 4, high = (tid & 4) << 4;  // the swizzle's bits
 #pragma unroll 1
             for (int x = 0; x < D / 32; ++x) {
-                const uint4 q = load16(at + x * p.bs * 16);
+                const uint4 q = load16(at + x * bs * 16);
                 const uint32_t w[4] = {q.x, q.y, q.z, q.w};
                 const uint32_t to = row + (x >> 1) * 1024 + (((x & 1) << 6) ^ high);
 #pragma unroll
-                for (int y = 0; y < 4; ++y)
-                    store16(to + ((y << 4) ^ low), q4::fma_bf16x2(q4::open_pair(w[y], 0, mask, ones), scale, offset), q4::fma_bf16x2(q4::open_pair(w[y], 1, mask, ones), scale, offset),
-                            q4::fma_bf16x2(q4::open_pair(w[y], 2, mask, ones), scale, offset), q4::fma_bf16x2(q4::open_pair(w[y], 3, mask, ones), scale, offset));
+                for (int y = 0; y < 4; ++y) open(to + ((y << 4) ^ low), w[y], scale, offset);
             }
         } else {
-            const int left = is_page(entry) ? c.seq_len - (c.tile_begin + j) * kTileTokens - t0 : 0;  // valid tokens of the thread's
-            entry = entry_of(j + 1);
-            const uint32_t at = my_codes + stage * Sh::kCodeBytes, pat = my_params + stage * Sh::kParamBytes;
-            const uint32_t col = dst + (cg >> 3) * 1024;
-            uint32_t words[kVTok / 8][8];  // of eight tokens of each channel
-            if constexpr (D == 128) {  // (64 bytes a thread; one word at a time 16 lanes would meet in a bank)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const uint4 q = load16(at + x * 16);
-                    words[0][2 * x] = q.x; words[1][2 * x] = q.y; words[0][2 * x + 1] = q.z; words[1][2 * x + 1] = q.w;
-                }
-            } else {
-#pragma unroll
-                for (int y = 0; y < 8; ++y) words[0][y] = load4(at + y * 8);
-            }
-#pragma unroll
-            for (int g = 0; g < kVTok / 8; ++g) {
-                uint32_t (&w)[8] = words[g];
-                const uint32_t rows = col + ((t0 >> 3) + g) * Sh::kGroupBytes;
-#pragma unroll 1
-                for (int x = 0; x < 8; x += 4) {  // tokens t0 + 8 g + x .. + 3
-                    uint32_t sc[2], of[2];
-                    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(sc[0]), "=r"(sc[1]) : "r"(pat + g * 16 + x * 2) : "memory");
-                    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(of[0]), "=r"(of[1]) : "r"(pat + two_bs + g * 16 + x * 2) : "memory");
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const int n = left - 8 * g - x - 2 * u;
-                        const uint32_t keep = n > 1 ? ~0u : n > 0 ? 0xFFFFu : 0u;  // a token that is not there: no scale, no offset, no value
-                        sc[u] &= keep;
-                        of[u] &= keep;
-                        uint32_t even[4], odd[4];
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) {  // channels 2 y and 2 y + 1 of the eight
-                            const uint32_t a = q4::fma_bf16x2(q4::open_pair(w[2 * y], u, mask, ones), sc[u], of[u]), z = q4::fma_bf16x2(q4::open_pair(w[2 * y + 1], u, mask, ones), sc[u], of[u]);
-                            even[y] = __byte_perm(a, z, 0x5410);
-                            odd[y] = __byte_perm(a, z, 0x7632);
-                        }
-                        const int t = x + 2 * u;
-                        store16(rows + t * 128 + (((cg & 7) ^ t) << 4), even[0], even[1], even[2], even[3]);
-                        store16(rows + t * 128 + 128 + (((cg & 7) ^ (t + 1)) << 4), odd[0], odd[1], odd[2], odd[3]);
+            const uint32_t stage_codes = codes + stage * Sh::kCodeBytes, stage_params = params + stage * Sh::kParamBytes;
+            const uint32_t in_page = (uint32_t)bs - 1, my_codes = stage_codes + (uint32_t)bs * (D / 2) + channel * 8;
+            const int n_valid = c.seq_len - (c.tile_begin + j) * kTileTokens;
+            const uint32_t bad = __ballot_sync(0xffffffffu, lane < ppt && lane * bs < n_valid && !is_page(v_entry));
+            v_entry = entry_of(j + 1, min(lane, ppt - 1));
+            if (n_valid < kTileTokens || bad) {  // every warp writes the zeros that it will read (the same ones)
+                for (int t = lane; t < kTileTokens; t += 32)
+                    if (t >= n_valid || (bad >> (t / bs) & 1)) {
+                        const uint32_t at = stage_params + t / bs * bs * 4 + t % bs * 2;
+                        asm volatile("st.shared.b16 [%0], %1;\n\tst.shared.b16 [%2], %1;" ::"r"(at), "h"((uint16_t)0), "r"(at + two_bs) : "memory");
                     }
-#pragma unroll
-                    for (int y = 0; y < 8; ++y) w[y] = __funnelshift_r(w[y], w[y], 8);
-                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before the stage is filled again
+                __syncwarp();
+            }
+#pragma unroll 4
+            for (int u = v_unit0; u < v_unit0 + kUnits; ++u) {  // 16 tokens: two words of codes
+                const uint32_t at = (uint32_t)u * 16 & in_page, page0 = (uint32_t)u * 16 & ~in_page;  // in the page; its first token
+                uint32_t w0, w1;
+                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w0), "=r"(w1) : "r"(my_codes + page0 * D + at * (D / 2)) : "memory");
+                const uint32_t par = stage_params + page0 * 4 + at * 2, to = v_row + (u >> 2) * (D * 128);
+                open(to + (((u & 3) << 5) ^ v_swizzle), w0, load16(par), load16(par + two_bs));
+                open(to + (((u & 3) << 5 | 16) ^ v_swizzle), w1, load16(par + 16), load16(par + two_bs + 16));
             }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) {
             mbar_arrive(smem_u32(&bars.kv_full[slot]));
-            if (!step) mbar_arrive(smem_u32(&bars.code_empty[stage]));
+            if (!step && (kV || kDo == kOpenK)) mbar_arrive(smem_u32(&bars.code_empty[stage]));
         }
+        return true;
+    };
+#pragma unroll 1
+    for (int j = 0; j < c.n_tiles; ++j) {
+        if constexpr ((kDo & kOpenK) != 0)
+            if (!tile(std::false_type(), j)) return;
+        if constexpr ((kDo & kOpenV) != 0)
+            if (!tile(std::true_type(), j)) return;
     }
 }
 
@@ -414,6 +410,10 @@ __device__ __forceinline__ void issue(const TcParams& p, const Job& c, Barriers&
         const uint32_t a = tmem + t * 128, d = tmem + 256 + t * 128;
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) {  // 16 tokens per instruction: two groups
+            if constexpr (kQ4) {  // rows of channels, 64 tokens each
+                mma_ts_lohi(d, a + kk * 8, vb_lo + (uint32_t)(((kk >> 2) * D * 128 + (kk & 3) * 32) >> 4), q_hi, make_idesc(D, false), (!first || kk > 0) ? 1u : 0u);
+                continue;
+            }
             const uint32_t b = vb_lo + (uint32_t)kk * (2 * Sh::kGroupBytes >> 4);
             mma_ts_lohi(d, a + kk * 8, b, kv_hi, kIdescPV<D>, (!first || kk > 0) ? 1u : 0u);
             if (kSplit) mma_ts_lohi(d, a + 64 + kk * 8, b, kv_hi, kIdescPV<D>, 1u);
@@ -892,9 +892,10 @@ __device__ __forceinline__ void softmax(const TcParams& p, const Job& c, Barrier
 // kForm: the row groups a launch can meet (a kernel with both forms has twice the code, which a call that follows other
 // kernels pays for in instruction-cache misses).
 enum { kOneTile, kTwoTiles, kBoth };
-// kQ4: the cache is one in 4 bits; eight more warps (open_tiles) fill the ring.
+// kQ4: the cache is one in 4 bits; four or eight more warps (open_tiles) fill the ring.
+constexpr int openers(int form, bool q4) { return !q4 ? 0 : form == kOneTile ? 8 : 4; }
 template <int D, int kForm, bool kSplit, bool kQ4>
-__global__ void __launch_bounds__(kQ4 ? kThreadsTc + 256 : kThreadsTc, 1) attn_tc_kernel(const __grid_constant__ TcParams p) {
+__global__ void __launch_bounds__(kThreadsTc + 32 * openers(kForm, kQ4), 1) attn_tc_kernel(const __grid_constant__ TcParams p) {
     using Sh = Shape<D, kQ4>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ Barriers bars;
@@ -943,7 +944,7 @@ __global__ void __launch_bounds__(kQ4 ? kThreadsTc + 256 : kThreadsTc, 1) attn_t
             bars.odd = 0;
             for (int x = 0; x < 2; ++x) {
                 mbar_init(smem_u32(&bars.code_full[x]), 1);
-                mbar_init(smem_u32(&bars.code_empty[x]), 8);
+                mbar_init(smem_u32(&bars.code_empty[x]), openers(kForm, kQ4));
             }
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -956,7 +957,7 @@ __global__ void __launch_bounds__(kQ4 ? kThreadsTc + 256 : kThreadsTc, 1) attn_t
     }
     if (c.tile_rows < 128) {  // rows past the packed ones are never copied: finite values, so that their softmax stays quiet
         const int n = (128 - c.tile_rows) * 8;
-        for (int i = threadIdx.x; i < 2 * Sh::kParts * n; i += kQ4 ? kThreadsTc + 256 : kThreadsTc)
+        for (int i = threadIdx.x; i < 2 * Sh::kParts * n; i += kThreadsTc + 32 * openers(kForm, kQ4))
             *reinterpret_cast<uint4*>(c.smem + (i / n) * 16384 + c.tile_rows * 128 + (i % n) * 16) = make_uint4(0, 0, 0, 0);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -995,7 +996,7 @@ __global__ void __launch_bounds__(kQ4 ? kThreadsTc + 256 : kThreadsTc, 1) attn_t
 
     if (work && c.n_tiles == 0) {
         // an empty split: publish (m = -inf, l = 0) so that the merge ignores it
-        for (int r = threadIdx.x; r < p.rg_tiles * 128; r += kQ4 ? kThreadsTc + 256 : kThreadsTc) {
+        for (int r = threadIdx.x; r < p.rg_tiles * 128; r += kThreadsTc + 32 * openers(kForm, kQ4)) {
             const size_t prow = (((size_t)c.lb * p.Hkv + c.h) * p.n_splits + c.split) * p.R_pad + c.rg * p.rg_tiles * 128 + r;
             p.part_ml[prow * 2] = -INFINITY;
             p.part_ml[prow * 2 + 1] = 0.f;
@@ -1004,7 +1005,7 @@ __global__ void __launch_bounds__(kQ4 ? kThreadsTc + 256 : kThreadsTc, 1) attn_t
     }
 
     if constexpr (kQ4) {
-        // Registers: 128 x 48 + 256 x 168 + 256 x 48 are the 640 x 96 of the launch
+        // Registers: 128 x 48 + 256 x 192 + 128 x 80 are the 512 x 128 of the launch, 128 x 48 + 256 x 168 + 256 x 48 the 640 x 96
         if (work) {
             if (warp < 4) {
                 asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
@@ -1014,10 +1015,19 @@ __global__ void __launch_bounds__(kQ4 ? kThreadsTc + 256 : kThreadsTc, 1) attn_t
                 }
                 if (warp == 1) one ? issue<D, true, kSplit, true>(p, c, bars, lane) : issue<D, false, kSplit, true>(p, c, bars, lane);
             } else if (warp >= 12) {
-                asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-                warp < 16 ? open_tiles<D, false>(p, c, bars, one, threadIdx.x - kThreadsTc) : open_tiles<D, true>(p, c, bars, one, threadIdx.x - kThreadsTc - 128);
+                if constexpr (openers(kForm, kQ4) == 4) {
+                    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+                    open_tiles<D, kOpenK | kOpenV>(p, c, bars, one, threadIdx.x - kThreadsTc);
+                } else {
+                    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+                    warp < 16 ? open_tiles<D, kOpenK>(p, c, bars, one, threadIdx.x - kThreadsTc)
+                              : open_tiles<D, kOpenV>(p, c, bars, one, threadIdx.x - kThreadsTc - 128);
+                }
             } else {
-                asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+                if constexpr (openers(kForm, kQ4) == 4)
+                    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+                else
+                    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
                 one ? softmax<D, true, kSplit, true>(p, c, bars, warp, lane) : softmax<D, false, kSplit, true>(p, c, bars, warp, lane);
             }
         }
@@ -1133,7 +1143,7 @@ template <int D, int kForm, bool kSplit, bool kQ4>
 specpv_status launch_form(const TcParams& p, int n_lb, cudaStream_t stream) {
     using Sh = Shape<D, kQ4>;
     if (!set_smem_limit_once(reinterpret_cast<const void*>(attn_tc_kernel<D, kForm, kSplit, kQ4>), Sh::kSmemBytes)) return SPECPV_ERR_CUDA;
-    if (launch_pdl(attn_tc_kernel<D, kForm, kSplit, kQ4>, p.n_splits * p.n_row_groups * p.Hkv * n_lb, kQ4 ? kThreadsTc + 256 : kThreadsTc,
+    if (launch_pdl(attn_tc_kernel<D, kForm, kSplit, kQ4>, p.n_splits * p.n_row_groups * p.Hkv * n_lb, kThreadsTc + 32 * openers(kForm, kQ4),
                    Sh::kSmemBytes, stream, p) != cudaSuccess)
         return SPECPV_ERR_CUDA;
     count_launch();
@@ -1261,6 +1271,8 @@ specpv_status launch_attention_tc(const AttnArgs& a, cudaStream_t stream) {
     // 32.5 -> 29.2 us).  Down to one tile per CTA pays (24 rows x 4, 2048 tokens: 15.8 / 15.1 / 14.2 us at 6 / 9 / 18
     // splits).  A last row group of one tile makes shorter CTAs, which come last in the grid (64K tokens x 36 layers,
     // 90 rows x 4: 4100 -> 3690 us).
+    // Over a cache in 4 bits a tile costs 2.1 and 2.6, bound by opening its codes (with the figures above: one layer, 60 rows x 4,
+    // 16384 tokens 44.8 instead of 38.1 us; 64K tokens x 8 layers 601 instead of 560 us).
     const int tok_per_tile = 128 / G, row_tiles = (a.M_max + tok_per_tile - 1) / tok_per_tile;
     const int n_units = Hkv * a.n_layers * a.batch;
     const int positions = (a.max_seq_len + kTileTokens - 1) / kTileTokens + 1;  // context tiles + the tile of the step's own tokens
@@ -1271,13 +1283,14 @@ specpv_status launch_attention_tc(const AttnArgs& a, cudaStream_t stream) {
     char* ws = reinterpret_cast<char*>(a.workspace) + a.partial_off;
     const size_t skip = (32 - (reinterpret_cast<uintptr_t>(ws) & 31)) & 31;
     const double scratch = (double)a.partial_bytes - (double)skip;
+    const double tile1 = a.q4_pool ? 2.1 : 0.9, tile2 = a.q4_pool ? 2.6 : 1.5;
     double best_cost = 1e30;
     for (int rg_tiles = row_tiles > 1 ? 2 : 1; rg_tiles >= 1; --rg_tiles) {
         const int groups = (row_tiles + rg_tiles - 1) / rg_tiles, full = row_tiles / rg_tiles;
         for (int s = 1; s <= 64 && s <= positions; ++s) {
             if (s > 1 && tile_bytes * s * groups * rg_tiles > scratch) break;
             const int tiles = (positions + s - 1) / s;
-            const double t1 = 7.0 + 0.9 * tiles + (s > 1 ? 1.5 : 0.0), t2 = 7.0 + 1.5 * tiles + (s > 1 ? 4.0 : 0.0);
+            const double t1 = 7.0 + tile1 * tiles + (s > 1 ? 1.5 : 0.0), t2 = 7.0 + tile2 * tiles + (s > 1 ? 4.0 : 0.0);
             const long long n_long = (long long)n_units * s * full, n_short = (long long)n_units * s * (groups - full);
             double cost = cta_makespan(n_long, rg_tiles == 2 ? t2 : t1, n_short, t1);
             if (s > 1) cost += 3.0 + row_bytes * s * 2.0 / 5.3e6;  // written and read through L2 at 5.3 TB/s
