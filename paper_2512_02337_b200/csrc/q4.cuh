@@ -60,46 +60,60 @@ __device__ __forceinline__ float value_of(uint32_t w, int e, uint16_t scale, uin
 }
 
 // A row's scale and offset from its smallest and largest element, and the code of an element.  A row whose range or offset bfloat16
-// cannot hold (an element that is infinite or NaN among them) is stored as NaN.
+// cannot hold is stored as NaN, and so is one whose `lo` or `hi` is infinite or NaN.
 struct Row {
     float scale, base;  // in float32, for the codes; base = what code 0 stands for before its rounding
     uint16_t scale16, offset16;
 };
-__device__ __forceinline__ Row row_of(float lo, float hi, bool finite) {
+// (x - base) / scale, and a range / 15, are IEEE quotients, in float32 to nearest.  So is RN(q + r i) with i a reciprocal of the divisor b
+// good to 2^-22 of itself, q = RN(a i) and r = a - q b: the dividend a has 24 significant bits and b at most 8 (it is a bfloat16, or 15), so that
+// r, 2^-21 of a at most and a multiple of the last places of q and b, has 12 bits and is exact; q + r i is then a / b but for 2^-43 of it, and
+// nearer than 2^-33 of itself a / b comes to no number half-way between two of float32: such a number has 25 bits, its product with b a
+// last place 2^-33 of it or more, and is not a, which would have 25 bits as well.  Outside of kLeast .. kMost, where the reciprocal or the remainder
+// may underflow, they are divided.
+constexpr float kLeast = 1e-30f, kMost = 1e30f;
+__device__ __forceinline__ float reciprocal(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float quotient(float a, float b, float inv) {
+    const float q = __fmul_rn(a, inv);
+    return __fmaf_rn(__fmaf_rn(-q, b, a), inv, q);
+}
+__device__ __forceinline__ Row row_of(float lo, float hi) {
     Row r;
-    const __nv_bfloat16 s = __float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f));
+    const float range = __fsub_rn(hi, lo);
+    const __nv_bfloat16 s = __float2bfloat16_rn(range > kLeast && range < kMost ? quotient(range, 15.f, 1.f / 15.f) : __fdiv_rn(range, 15.f));
     r.scale = __bfloat162float(s);
     const __nv_bfloat16 c = __float2bfloat16_rn(__fsub_rn(lo, 16.f * r.scale));  // (16 s is exact)
     const float offset = __bfloat162float(c);
     r.base = __fadd_rn(offset, 16.f * r.scale);
     r.scale16 = __bfloat16_as_ushort(s);
     r.offset16 = __bfloat16_as_ushort(c);
-    if (!finite || !isfinite(r.scale) || !isfinite(offset) || !isfinite(r.base)) {
+    if (!isfinite(r.scale) || !isfinite(offset) || !isfinite(r.base)) {
         r.scale = r.base = __int_as_float(0x7FC00000);
         r.scale16 = r.offset16 = 0x7FC0;
     }
     return r;
 }
-// Codes of a lane's elements: the nearest integers of (x - base) / scale, ties to even, by IEEE division.  A multiplication by the
-// reciprocal is off by some 2^-23 of at most 16, so that it names another integer only next to a tie: where it comes that near (or the
-// reciprocal is not to be trusted) the warp divides after all.
-template <int N>
-__device__ __forceinline__ void codes_of(const Row& r, const float (&x)[N], uint32_t (&codes)[N]) {
-    const float inv = __frcp_rn(r.scale);
-    bool exact = !(r.scale > 1e-37f);  // (a row of equal elements, or one that is NaN, among them)
+// The codes of eight elements as a word before its rotation: the nearest integers of (x - base) / scale, ties to even, 0 to 15.
+__device__ __forceinline__ uint32_t word_of(const Row& r, const float (&x)[8]) {
+    constexpr float kWhole = 12582912.f;  // 1.5 2^23: what is added to it is rounded to an integer, its last bits
+    constexpr uint32_t kWholeBits = 0x4B400000u;
+    const float inv = reciprocal(r.scale);
+    float m[8];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float q = fminf(fmaxf(__fsub_rn(x[i], r.base) * inv, 0.f), 15.f), m = q + 12582912.f;  // 1.5 2^23: rounds to an integer
-        exact |= fabsf(q - (m - 12582912.f)) > 0.4999f;
-        codes[i] = __float_as_uint(m) & 15u;
-    }
-    if (__any_sync(0xffffffffu, exact)) {
+    for (int i = 0; i < 8; ++i) m[i] = __fadd_rn(fminf(fmaxf(quotient(__fsub_rn(x[i], r.base), r.scale, inv), 0.f), 15.f), kWhole);
+    if (!(r.scale > kLeast && r.scale < kMost)) {  // (rows of equal elements, and NaN, among these)
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float n = rintf(__fdiv_rn(__fsub_rn(x[i], r.base), r.scale));
-            codes[i] = (uint32_t)fminf(fmaxf(n, 0.f), 15.f);  // 0 / 0: fmaxf takes the 0
-        }
+        for (int i = 0; i < 8; ++i)  // 0 / 0: fmaxf takes the 0
+            m[i] = __fadd_rn(fminf(fmaxf(__fdiv_rn(__fsub_rn(x[i], r.base), r.scale), 0.f), 15.f), kWhole);
     }
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w += (__float_as_uint(m[e]) - kWholeBits) << element_shift(e);
+    return w;
 }
 
 }  // namespace q4
