@@ -31,14 +31,16 @@ __device__ __forceinline__ void mma_tf32(float (&c)[4], uint32_t a0, uint32_t a1
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// x as two terms of 11 bits; an infinity or NaN goes into the first alone
-__device__ __forceinline__ void two_terms(uint32_t x, uint32_t& hi, uint32_t& lo) {
+// x as two terms of 11 bits.  An infinity or NaN is the first alone, and `finite`, what the other factor's second term meets, is then 0:
+// its products are those with the other's first term, which has the sign and is zero only where the factor is.
+__device__ __forceinline__ void two_terms(uint32_t x, uint32_t& hi, uint32_t& finite, uint32_t& lo) {
     asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(__uint_as_float(x)));
     const float rest = __uint_as_float(x) - __uint_as_float(hi);
     asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(lo) : "f"(rest));
+    finite = hi;
     if ((x & 0x7F800000u) == 0x7F800000u) {
         hi = x;
-        lo = 0;
+        finite = lo = 0;
     }
 }
 
@@ -57,12 +59,16 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
     const int rows = min(p.row1, n * p.G) - p.row0, row_tiles = (rows + 7) / 8;
     if (tile0 >= tile1 || rows <= 0) return;
     uint4* s_q = reinterpret_cast<uint4*>(acc_smem);  // [row tile][piece][lane]
-    float* s_lse = reinterpret_cast<float*>(s_q + row_tiles * kPieces * 32);  // [row], log2; +infinity adds nothing
-    int* s_end = reinterpret_cast<int*>(s_lse + row_tiles * 8);  // tokens that the row sees
+    float* s_lse = reinterpret_cast<float*>(s_q + row_tiles * kPieces * 32);  // [row], log2
+    int* s_end = reinterpret_cast<int*>(s_lse + row_tiles * 8);  // tokens that the row sees: none, if it adds nothing
+    __shared__ uint32_t s_idle;                               // bit per row tile: such rows are among it
+    static_assert(kAccPassRows / 8 <= 32, "a bit per row tile");
+    if (threadIdx.x == 0) s_idle = 0;
+    __syncthreads();
     for (int i = threadIdx.x; i < row_tiles * 8; i += 32 * kAccWarps) {
         const int r = p.row0 + i, a = r / p.G;
-        float lse = INFINITY;
-        int row = -1;
+        float lse = 0.f;
+        int row = -1, end = -1;
         if (i < rows) {
             row = p.accepted ? p.accepted[(size_t)b * p.A_max + a] : a;
             if (row < 0 || row >= p.M_max) {
@@ -70,11 +76,15 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
                 row = -1;
             } else {
                 lse = p.lse[((size_t)lb * p.M_max + row) * p.Hq + h * p.G + r % p.G] * 1.4426950408889634f;
-                if (lse == -INFINITY) lse = INFINITY;
+                if (lse == -INFINITY)
+                    lse = 0.f;
+                else
+                    end = seq_len - n + a + 1;
             }
         }
+        if (end < 0) atomicOr(&s_idle, 1u << (i >> 3));
         s_lse[i] = lse;
-        s_end[i] = seq_len - n + a + 1;
+        s_end[i] = end;
         const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.q) + (((size_t)lb * p.M_max + max(row, 0)) * p.Hq + h * p.G + r % p.G) * D);
 #pragma unroll
         for (int j = 0; j < kPieces; ++j)
@@ -83,6 +93,7 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
                 s_q[((i >> 3) * kPieces + j) * 32 + (i & 7) * 4 + x] = row < 0 ? make_uint4(0, 0, 0, 0) : src[j * 4 + x];
     }
     __syncthreads();
+    const uint32_t idle = s_idle;
     const uint4* k_pool = reinterpret_cast<const uint4*>(p.k_pool) + ((size_t)(p.layer0 + l) * p.n_pages * p.Hkv + h) * p.bs * (D * sizeof(T) / 16);
     const size_t page_stride = (size_t)p.Hkv * p.bs * (D * sizeof(T) / 16);
     const int32_t* table = p.block_table + (size_t)b * p.max_blocks;
@@ -137,15 +148,15 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
                     const uint32_t qw[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
                     for (int x = 0; x < 4; x += 2) {
-                        uint32_t ah[4], al[4], bh[2], bl[2];
-                        two_terms(k[0][4 * j + x], ah[0], al[0]);
-                        two_terms(k[1][4 * j + x], ah[1], al[1]);
-                        two_terms(k[0][4 * j + x + 1], ah[2], al[2]);
-                        two_terms(k[1][4 * j + x + 1], ah[3], al[3]);
-                        two_terms(qw[x], bh[0], bl[0]);
-                        two_terms(qw[x + 1], bh[1], bl[1]);
-                        mma_tf32(c, al[0], al[1], al[2], al[3], bh[0], bh[1]);
-                        mma_tf32(c, ah[0], ah[1], ah[2], ah[3], bl[0], bl[1]);
+                        uint32_t ah[4], af[4], al[4], bh[2], bf[2], bl[2];
+                        two_terms(k[0][4 * j + x], ah[0], af[0], al[0]);
+                        two_terms(k[1][4 * j + x], ah[1], af[1], al[1]);
+                        two_terms(k[0][4 * j + x + 1], ah[2], af[2], al[2]);
+                        two_terms(k[1][4 * j + x + 1], ah[3], af[3], al[3]);
+                        two_terms(qw[x], bh[0], bf[0], bl[0]);
+                        two_terms(qw[x + 1], bh[1], bf[1], bl[1]);
+                        mma_tf32(c, al[0], al[1], al[2], al[3], bf[0], bf[1]);
+                        mma_tf32(c, af[0], af[1], af[2], af[3], bl[0], bl[1]);
                         mma_tf32(c, ah[0], ah[1], ah[2], ah[3], bh[0], bh[1]);
                     }
                 }
@@ -153,7 +164,7 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
             const float2 lse = *reinterpret_cast<const float2*>(s_lse + rt * 8 + 2 * t);
             float w[4] = {tc::ex2(fmaf(c[0], scale, -lse.x)), tc::ex2(fmaf(c[1], scale, -lse.y)), tc::ex2(fmaf(c[2], scale, -lse.x)),
                           tc::ex2(fmaf(c[3], scale, -lse.y))};
-            if (!all_seen) {
+            if (!all_seen || (idle >> rt & 1)) {  // (by choice, not by a weight of 0: the key may be infinite)
                 const int2 end = *reinterpret_cast<const int2*>(s_end + rt * 8 + 2 * t);
                 if (token >= end.x) w[0] = 0.f;
                 if (token >= end.y) w[1] = 0.f;

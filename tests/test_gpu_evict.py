@@ -113,6 +113,38 @@ def test_account_of_no_rows_empty_rows_and_an_empty_cache():
     run_accumulate("fp32", 8, 2, 64, 16, 4, [100], [[2, 3]], 3, empty_row=True, scale=0.3)
 
 
+def test_account_of_one_row_many_times():
+    run_accumulate("bf16", 8, 2, 128, 64, 4, [100], [[2, 2, 2]], 3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("A", [1, 3])
+def test_account_of_infinite_keys(dtype, A):
+    """A score of -infinity adds nothing, one of +infinity an infinity, and both to their own token alone; rows that are not there, and
+    those whose lse is -infinity, add nothing even so."""
+    rng = np.random.default_rng(A)
+    cfg = config(1, 2, 1, 64, 16, dtype)
+    cache, k64, _ = make_cache(1, 1, 64, 16, [50], dtype, rng)
+    q = torch.from_numpy(rng.standard_normal((1, 1, 4, 2, 64))).to(torch_dtype(dtype)).cuda()
+    q[..., 7] = -q[..., 7].abs() - 0.5
+    q[..., 9] = 1.0
+    page, at = cache.block_table[0, 1].item(), 3
+    cache.k_pool[0, page, 0, at, 7] = float("inf")       # token 19
+    cache.k_pool[0, page, 0, at + 1, 7] = -float("inf")  # token 20
+    cache.k_pool[0, page, 0, at + 2, 9] = -float("inf")  # token 21
+    lse = torch.full((1, 1, 4, 2), 5.0, device="cuda")
+    lse[0, 0, 2] = -float("inf")
+    acc = torch.ones(1, 1, 1, 64, device="cuda")
+    ws = B.new_workspace(cfg, 1, 1, 64, 4)
+    n = torch.tensor([A], dtype=torch.int32, device="cuda")
+    B.specpv_accumulate_attention(cfg, 0, 1, q, lse, 4, None, n, A, cache, acc, ws)
+    assert B.specpv_poll_status(ws)[0] == 0
+    a = acc[0, 0, 0].cpu().numpy()
+    assert a[19] == 1.0 and a[20] == np.inf and a[21] == 1.0
+    assert np.all(np.isfinite(np.delete(a, 20))) and np.all(a[50:] == 1.0)
+    assert np.all(np.delete(a[: 50 - A], [19, 20, 21]) > 1.0)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_account_faults_are_reported(dtype):
     rng = np.random.default_rng(0)
