@@ -32,7 +32,7 @@ constexpr int kChunk = 64;               // tokens
 // Rows of a KV head; also bounds the step's tokens, which are one chunk.  (us, 65536 tokens x 8 layers, 4 / 8 / 16 rows of 128 here 145 / 146 /
 // 241, on the tcgen05 kernel 457 / 483 / 485; 32 rows in one CTA 552, as two CTAs of 16 459, there 486; 4096 tokens x 1 layer 43 / 26, there 16.)
 constexpr int kMaxRows = 16;
-constexpr float kRaise = 60.f;           // log2 of the weight from which references are raised
+constexpr float kRaise = 16.f;           // log2 of the weight from which references are raised
 
 // rows of a CTA: 8 NT
 template <int D, int NT>
@@ -305,7 +305,8 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
             }
         }
         // A row's reference is its largest score in the warp's first chunk (looked at once more where its scores are not all in
-        // registers together).  It is raised when a weight passes 2^60 (float32 sums and bfloat16 weights keep their relative precision at any exponent).
+        // registers together).  It is raised when a weight passes 2^16: float32 sums and bfloat16 weights
+        // keep their relative precision at any exponent, and values as large as 2^100 are not carried past float32.
         bool look = i == 0;
         auto reference = [&](float most) {
 #pragma unroll
