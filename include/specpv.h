@@ -363,7 +363,8 @@ specpv_status specpv_verify_full_offloaded(const specpv_config *cfg, int layer0,
  *          key codes [d / 32][bs][16 bytes] | value codes [bs / 16][d][8 bytes] | [4][bs] bfloat16: key scales, key offsets, value
  *          scales, value offsets.  A 32-bit word holds eight codes, of consecutive channels (keys) or tokens (values): element 2 i in
  *          bits 4 i .. 4 i + 3, element 2 i + 1 in bits 16 + 4 i .. 19 + 4 i, the word then rotated left by three bits.
- * The step's own tensors (q, k_new, v_new, out) are of cfg->dtype, as everywhere. */
+ * The step's own tensors (q, k_new, v_new, out) are of cfg->dtype, as everywhere.  A call takes at most 65535 (layer, sequence) pairs
+ * (SPECPV_ERR_CAPACITY); the same holds for the account and the eviction below. */
 typedef struct {
     void *pool;                 /* device */
     const int32_t *block_table; /* device, [batch][max_blocks] */

@@ -67,8 +67,13 @@ static specpv_status validate_q4(const Geometry& g, const specpv_paged_q4* kv) {
     if (!kv || !kv->pool || !kv->block_table || !kv->seq_lens) return SPECPV_ERR_INVALID_ARG;
     if (!aligned16(kv->pool)) return SPECPV_ERR_INVALID_ARG;
     if (kv->batch <= 0 || kv->max_blocks <= 0 || kv->n_pages <= 0 || kv->max_seq_len < 0) return SPECPV_ERR_INVALID_ARG;
-    if ((int64_t)kv->max_seq_len > (int64_t)kv->max_blocks * g.bs) return SPECPV_ERR_CAPACITY;
+    if ((int64_t)kv->max_seq_len > (int64_t)kv->max_blocks * g.bs || (int64_t)kv->max_blocks * g.bs > INT32_MAX) return SPECPV_ERR_CAPACITY;
     return SPECPV_OK;
+}
+
+// what the launches over (layer, sequence) pairs and over the rows of a step can number
+static bool in_reach(const Geometry& g, int n_layers, int batch, int rows) {
+    return (int64_t)n_layers * batch <= 65535 && (int64_t)rows * g.G <= INT32_MAX / 2;
 }
 
 StagingPlan plan_staging(const Geometry& g, int n_layers_per_call, int batch, int M_max) {
@@ -622,7 +627,7 @@ SPECPV_EXPORT specpv_status specpv_verify_full_q4(const specpv_config* cfg, int 
     if (!q || !k_new || !v_new || !tree_mask || !out || !workspace) return SPECPV_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out) || !aligned16(workspace)) return SPECPV_ERR_INVALID_ARG;
     if (layer0 < 0 || n_layers <= 0 || layer0 + n_layers > g.n_layers || M_max <= 0) return SPECPV_ERR_INVALID_ARG;
-    if (M_max > kMaxQTokens) return SPECPV_ERR_CAPACITY;
+    if (M_max > kMaxQTokens || !in_reach(g, n_layers, full->batch, M_max)) return SPECPV_ERR_CAPACITY;
     const WorkspacePlan w = plan_workspace(g, n_layers, full->batch, M_max);
     if (workspace_bytes < w.partial_off + w.partial_bytes) return SPECPV_ERR_CAPACITY;
     AttnArgs a{};
@@ -654,7 +659,7 @@ SPECPV_EXPORT specpv_status specpv_commit_accepted_q4(const specpv_config* cfg, 
     if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_values) || !aligned16(v_values)) return SPECPV_ERR_INVALID_ARG;
     if ((kmax == nullptr) != (kmin == nullptr) || (k_values == nullptr) != (v_values == nullptr)) return SPECPV_ERR_INVALID_ARG;
     if (layer0 < 0 || n_layers <= 0 || layer0 + n_layers > g.n_layers || M_max <= 0 || A_max <= 0) return SPECPV_ERR_INVALID_ARG;
-    if (!accepted && A_max > M_max) return SPECPV_ERR_CAPACITY;
+    if ((!accepted && A_max > M_max) || !in_reach(g, n_layers, dst->batch, A_max)) return SPECPV_ERR_CAPACITY;
     CommitQ4Params p{};
     p.k_new = k_new; p.v_new = v_new; p.accepted = accepted; p.n_accepted = n_accepted; p.pool = dst->pool;
     p.block_table = dst->block_table; p.seq_lens = const_cast<int32_t*>(dst->seq_lens); p.kmax = kmax; p.kmin = kmin;
@@ -677,6 +682,7 @@ SPECPV_EXPORT specpv_status specpv_refresh_partial_q4(const specpv_config* cfg, 
     if (!idx || !count || !partial_lens || !workspace || workspace_bytes < kStatusBytes) return SPECPV_ERR_INVALID_ARG;
     if (partial->batch != full->batch || partial->n_pages <= 0) return SPECPV_ERR_INVALID_ARG;
     if ((int64_t)partial->max_blocks * g.bs < (int64_t)g.budget_blocks * g.bs + g.buffer_tokens) return SPECPV_ERR_CAPACITY;
+    if (!in_reach(g, g.n_layers, full->batch, 1)) return SPECPV_ERR_CAPACITY;
     GatherQ4Params p{};
     p.pool = full->pool; p.full_table = full->block_table; p.seq_lens = full->seq_lens; p.idx = idx; p.count = count;
     p.part_k = partial->k_pool; p.part_v = partial->v_pool; p.part_table = partial->block_table; p.partial_lens = partial_lens;
@@ -699,7 +705,8 @@ SPECPV_EXPORT specpv_status specpv_accumulate_attention(const specpv_config* cfg
     if (!q || !lse || !n_accepted || !acc || !workspace || workspace_bytes < kStatusBytes) return SPECPV_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(acc)) return SPECPV_ERR_INVALID_ARG;
     if (layer0 < 0 || n_layers <= 0 || layer0 + n_layers > g.n_layers || M_max <= 0 || A_max <= 0) return SPECPV_ERR_INVALID_ARG;
-    if (M_max > kMaxQTokens || (!accepted && A_max > M_max)) return SPECPV_ERR_CAPACITY;
+    if (M_max > kMaxQTokens || (!accepted && A_max > M_max) || !in_reach(g, n_layers, kv->batch, A_max)) return SPECPV_ERR_CAPACITY;
+    if ((int64_t)kv->max_blocks * g.bs > INT32_MAX) return SPECPV_ERR_CAPACITY;
     AccumulateParams p{};
     p.q = q; p.lse = lse; p.accepted = accepted; p.n_accepted = n_accepted; p.k_pool = kv->k_pool; p.block_table = kv->block_table;
     p.seq_lens = kv->seq_lens; p.acc = acc; p.workspace = workspace;
@@ -718,8 +725,7 @@ SPECPV_EXPORT specpv_status specpv_evict_tokens(const specpv_config* cfg, const 
     if (st != SPECPV_OK) return st;
     if (!acc || !idx || !workspace || workspace_bytes < kStatusBytes || !aligned16(acc)) return SPECPV_ERR_INVALID_ARG;
     if (sink_tokens < 0 || local_tokens < 0 || (int64_t)keep_tokens < (int64_t)sink_tokens + local_tokens + 1) return SPECPV_ERR_BUDGET;
-    if (kv->batch > 65535 || g.n_layers > 65535 || (int64_t)g.n_layers * kv->batch > 65535) return SPECPV_ERR_CAPACITY;
-    if ((int64_t)kv->max_blocks * g.bs > 0x7FFFFFFF) return SPECPV_ERR_CAPACITY;
+    if (!in_reach(g, g.n_layers, kv->batch, 1) || (int64_t)kv->max_blocks * g.bs > INT32_MAX) return SPECPV_ERR_CAPACITY;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     // a token is a block of one: the selection of blocks (ties, NaN, select_shared) serves as it is
     SelectParams c{};

@@ -159,3 +159,22 @@ def test_quantisation_is_off_by_half_a_step():
     # half a step; at the ends of the range, fifteen roundings of the scale; the offset's; the value's own
     assert np.all(np.abs(y - x) <= (s / 2 + 31 * s * Q.HALF_BF16 + np.abs(o) * Q.HALF_BF16)[:, None] + Q.HALF_BF16 * size[:, None])
     assert n.min() == 0 and n.max() == 15
+
+
+def test_what_launches_cannot_number_is_refused(env):
+    """More than 65535 (layer, sequence) pairs in a call, row counts and capacities past int32: an error before any launch."""
+    _, p, cfg = env
+    many, long = dict(batch=40000), dict(max_blocks=2 ** 31 // 16)
+    huge = 2 ** 31 - 1
+    lib, c = B.lib(), ctypes.byref(cfg)
+    for over in (many, long):
+        a, b = ctypes.byref(q4(p, **over)), ctypes.byref(kv(p, **over))
+        assert lib.specpv_verify_full_q4(c, 0, 2, p, p, p, p, None, 16, a, p, None, p, 1 << 40, None) == CAPACITY
+        assert lib.specpv_commit_accepted_q4(c, 0, 2, p, p, 16, p, p, 4, a, None, None, None, None, p, 4096, None) == CAPACITY
+        part = ctypes.byref(kv(p, **many)) if over is many else ctypes.byref(kv(p))
+        assert lib.specpv_refresh_partial_q4(c, a, p, p, part, p, p, 4096, None) == CAPACITY
+        assert lib.specpv_accumulate_attention(c, 0, 2, p, p, 16, p, p, 4, b, p, p, 4096, None) == CAPACITY
+        assert lib.specpv_evict_tokens(c, b, p, 64, 4, 8, p, p, 4096, None) == CAPACITY
+    a, b = ctypes.byref(q4(p)), ctypes.byref(kv(p))
+    assert lib.specpv_commit_accepted_q4(c, 0, 1, p, p, 16, p, p, huge, a, None, None, None, None, p, 4096, None) == CAPACITY
+    assert lib.specpv_accumulate_attention(c, 0, 1, p, p, 16, p, p, huge, b, p, p, 4096, None) == CAPACITY
