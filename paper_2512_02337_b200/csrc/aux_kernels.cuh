@@ -121,7 +121,8 @@ struct AccumulateParams {
     void* workspace;
     int layer0, batch, M_max, A_max, Hq, Hkv, G, bs, max_blocks, n_pages;
     float scale;
-    int tiles_per_cta, row0, row1;  // set by the launcher: 16-token tiles of a CTA; rows (accepted row * G + head) of the launch
+    // set by the launcher: 16-token tiles of a CTA, their number in a page (log2), rows (accepted row * G + head) of the launch
+    int tiles_per_cta, tiles_log2, row0, row1;
     int pdl;                        // set by launch_pdl_if
 };
 struct EvictParams {

@@ -99,68 +99,65 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
     const int32_t* table = p.block_table + (size_t)b * p.max_blocks;
     float* acc = p.acc + (((size_t)(p.layer0 + l) * p.batch + b) * p.Hkv + h) * (size_t)p.max_blocks * p.bs;
     const float scale = p.scale * 1.4426950408889634f;
-    auto entry_of = [&](int tile) { return tile < tile1 ? table[tile * kAccTokens / p.bs] : -1; };
-    uint4 next[2][kPieces];
-    bool next_ok = false;
-    auto fetch = [&](int tile, int page) {  // keys of tokens g and g + 8
-        next_ok = page >= 0 && page < p.n_pages;
-        if (tile >= tile1) return;
-        if (!next_ok) {
-            if (lane == 0) record_fault(p.workspace, SPECPV_ERR_BAD_BLOCK_TABLE, b, tile * kAccTokens / p.bs, page, l);
-            return;
+    // tiles of 16 tokens divide a page (of 16, 32 or 64): page and place by shifts
+    auto entry_of = [&](int tile) { return tile < tile1 ? table[tile >> p.tiles_log2] : -1; };
+    auto fetch = [&](int tile, int page, uint4 (&x)[2][kPieces]) {  // keys of tokens g and g + 8; whether they are there
+        if (tile >= tile1) return false;
+        if (page < 0 || page >= p.n_pages) {
+            if (lane == 0) record_fault(p.workspace, SPECPV_ERR_BAD_BLOCK_TABLE, b, tile >> p.tiles_log2, page, l);
+            return false;
         }
-        const uint4* src = k_pool + page * page_stride + (size_t)(tile * kAccTokens % p.bs + g) * (D * sizeof(T) / 16) + t;
+        const int at = (tile & ((1 << p.tiles_log2) - 1)) * kAccTokens + g;
+        const uint4* src = k_pool + page * page_stride + at * (int)(D * sizeof(T) / 16) + t;
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
-            for (int j = 0; j < kPieces; ++j) next[r][j] = src[r * 8 * (D * sizeof(T) / 16) + j * 4];
+            for (int j = 0; j < kPieces; ++j) x[r][j] = src[r * 8 * (D * sizeof(T) / 16) + j * 4];
+        return true;
     };
     int tile = tile0 + warp;
+    uint4 buf[2][2][kPieces];
+    bool there = fetch(tile, entry_of(tile), buf[0]);
     int entry = entry_of(tile + kAccWarps);
-    fetch(tile, entry_of(tile));
-    for (; tile < tile1; tile += kAccWarps) {
-        uint32_t k[2][kPieces * 4];
-#pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-            for (int j = 0; j < kPieces; ++j) {
-                k[r][4 * j] = next[r][j].x; k[r][4 * j + 1] = next[r][j].y; k[r][4 * j + 2] = next[r][j].z; k[r][4 * j + 3] = next[r][j].w;
-            }
-        const bool ok = next_ok;
+    // `now` holds the tile's keys, `next` receives those of the warp's next tile meanwhile
+    auto work = [&](const uint4 (&now)[2][kPieces], uint4 (&next)[2][kPieces]) {
         const int token = tile * kAccTokens + g;
         float* mine = acc + token + 8 * t;  // of lanes t = 0 and 1
-        const bool writes = ok && t < 2 && token + 8 * t < seq_len;
+        const bool writes = there && t < 2 && token + 8 * t < seq_len;
         const float before = writes ? *mine : 0.f;
-        fetch(tile + kAccWarps, entry);
+        there = fetch(tile + kAccWarps, entry, next);
         entry = entry_of(tile + 2 * kAccWarps);
         const bool all_seen = (tile + 1) * kAccTokens <= seq_len - n;
         float sum[2] = {0.f, 0.f};
 #pragma unroll 1
         for (int rt = 0; rt < row_tiles; ++rt) {
-            float c[4] = {0.f, 0.f, 0.f, 0.f};
+            float c[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};  // two chains of products
 #pragma unroll
             for (int j = 0; j < kPieces; ++j) {
                 const uint4 q = s_q[(rt * kPieces + j) * 32 + lane];
+                const uint4 k0 = now[0][j], k1 = now[1][j];
                 if constexpr (!kF32) {
-                    mma_bf16(c, k[0][4 * j], k[1][4 * j], k[0][4 * j + 1], k[1][4 * j + 1], q.x, q.y);
-                    mma_bf16(c, k[0][4 * j + 2], k[1][4 * j + 2], k[0][4 * j + 3], k[1][4 * j + 3], q.z, q.w);
+                    mma_bf16(c, k0.x, k1.x, k0.y, k1.y, q.x, q.y);
+                    mma_bf16(c1, k0.z, k1.z, k0.w, k1.w, q.z, q.w);
                 } else {
-                    const uint32_t qw[4] = {q.x, q.y, q.z, q.w};
+                    const uint32_t kw[2][4] = {{k0.x, k0.y, k0.z, k0.w}, {k1.x, k1.y, k1.z, k1.w}}, qw[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
                     for (int x = 0; x < 4; x += 2) {
                         uint32_t ah[4], af[4], al[4], bh[2], bf[2], bl[2];
-                        two_terms(k[0][4 * j + x], ah[0], af[0], al[0]);
-                        two_terms(k[1][4 * j + x], ah[1], af[1], al[1]);
-                        two_terms(k[0][4 * j + x + 1], ah[2], af[2], al[2]);
-                        two_terms(k[1][4 * j + x + 1], ah[3], af[3], al[3]);
+                        two_terms(kw[0][x], ah[0], af[0], al[0]);
+                        two_terms(kw[1][x], ah[1], af[1], al[1]);
+                        two_terms(kw[0][x + 1], ah[2], af[2], al[2]);
+                        two_terms(kw[1][x + 1], ah[3], af[3], al[3]);
                         two_terms(qw[x], bh[0], bf[0], bl[0]);
                         two_terms(qw[x + 1], bh[1], bf[1], bl[1]);
-                        mma_tf32(c, al[0], al[1], al[2], al[3], bf[0], bf[1]);
-                        mma_tf32(c, af[0], af[1], af[2], af[3], bl[0], bl[1]);
+                        mma_tf32(c1, al[0], al[1], al[2], al[3], bf[0], bf[1]);
+                        mma_tf32(c1, af[0], af[1], af[2], af[3], bl[0], bl[1]);
                         mma_tf32(c, ah[0], ah[1], ah[2], ah[3], bh[0], bh[1]);
                     }
                 }
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c[e] += c1[e];
             const float2 lse = *reinterpret_cast<const float2*>(s_lse + rt * 8 + 2 * t);
             float w[4] = {tc::ex2(fmaf(c[0], scale, -lse.x)), tc::ex2(fmaf(c[1], scale, -lse.y)), tc::ex2(fmaf(c[2], scale, -lse.x)),
                           tc::ex2(fmaf(c[3], scale, -lse.y))};
@@ -180,6 +177,13 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
             sum[1] += __shfl_xor_sync(0xffffffffu, sum[1], o);
         }
         if (writes) *mine = before + (t ? sum[1] : sum[0]);
+        tile += kAccWarps;
+    };
+#pragma unroll 1
+    while (tile < tile1) {
+        work(buf[0], buf[1]);
+        if (tile >= tile1) break;
+        work(buf[1], buf[0]);
     }
 }
 
@@ -325,11 +329,21 @@ __global__ void __launch_bounds__(kLensThreads) evict_lens_kernel(EvictParams p)
 
 template <typename T, int D>
 static specpv_status launch_accumulate_typed(AccumulateParams p, int n_layers, int max_seq_len, cudaStream_t stream) {
-    // A warp should have a few tiles to hide its start behind, the launch CTAs enough to fill the SMs twice
+    // Tiles per warp: the waves of CTAs, two on an SM, times what one takes, of which a start is about two and a half tiles (32 layers x 8
+    // heads x 4261 tokens, 20 rows: 58 us with 14 tiles per warp, kNowUs with the 17 chosen).
     const long long tiles = (max_seq_len + kAccTokens - 1) / kAccTokens, heads = (long long)p.Hkv * n_layers * p.batch;
-    long long per_warp = tiles * heads / (kAccWarps * 4LL * 148);
-    per_warp = per_warp < 1 ? 1 : per_warp > 16 ? 16 : per_warp;
-    p.tiles_per_cta = (int)per_warp * kAccWarps;
+    int per_warp = 1;
+    double best = 1e300;
+    for (int w = 1; w <= 48; ++w) {
+        const long long ctas = heads * ((tiles + kAccWarps * w - 1) / (kAccWarps * w));
+        const double cost = (double)((ctas + 2 * 148 - 1) / (2 * 148)) * (w + 2.5);
+        if (cost < best) {
+            best = cost;
+            per_warp = w;
+        }
+    }
+    p.tiles_per_cta = per_warp * kAccWarps;
+    p.tiles_log2 = p.bs == 64 ? 2 : p.bs == 32 ? 1 : 0;
     const dim3 grid((unsigned)((tiles + p.tiles_per_cta - 1) / p.tiles_per_cta), p.Hkv, n_layers * p.batch);
     const int all_rows = p.A_max * p.G;
     for (p.row0 = 0; p.row0 < all_rows; p.row0 += kAccPassRows) {
