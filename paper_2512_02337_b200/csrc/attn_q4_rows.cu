@@ -126,473 +126,496 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
         per_head += __reduce_add_sync(0xffffffffu, n);
         longest = max(longest, __reduce_max_sync(0xffffffffu, n));
     }
-    const int total = per_head * p.Hkv * p.n_layers, least = (longest + p.n_slots - 2) / (p.n_slots - 1);
-    const int n_ctas = max(1, min((int)gridDim.x, total / max(least, 1)));
+    const int total = per_head * p.Hkv * p.n_layers;
+    int n_ctas = (int)gridDim.x, share = total / n_ctas;
+    if ((long long)share * (p.n_slots - 1) < longest) {
+        const int least = (longest + p.n_slots - 2) / (p.n_slots - 1);
+        n_ctas = max(1, min(n_ctas, total / least));
+        share = total / n_ctas;
+    }
     if ((int)blockIdx.x >= n_ctas) return;
-    // floor(total c / n_ctas) and its inverse (the last CTA whose share starts at or before a position); the quotients are no nearer
-    // than 1 / n_ctas to an integer that they are not, so that their floors are exact
-    auto share_at = [&](int c) { return (int)((double)total * c / n_ctas); };
-    auto cta_of = [&](int at) { return (int)(((double)(at + 1) * n_ctas - 1.0) / total); };
+    // floor(total c / n_ctas), which lies on a unit's edge wherever it can, and its inverse, the last CTA whose share starts at or
+    // before a position (a float32 guess, put right)
+    const int more = total - share * n_ctas;
+    const float per_position = (float)n_ctas / (float)total;
+    auto share_at = [&](int c) { return share * c + more * c / n_ctas; };
+    auto cta_of = [&](int at) {
+        int c = min((int)((float)at * per_position), n_ctas - 1);
+        while (share_at(c) > at) --c;
+        while (share_at(c + 1) <= at) ++c;
+        return c;
+    };
     int at = share_at(blockIdx.x);
     const int share_end = share_at(blockIdx.x + 1);
     uint32_t fills = 0;  // chunks that the warp has taken from its stages so far
     while (at < share_end) {
-    // ---- the unit at `at`, and the part of it that is the CTA's ----
-    const int l = at / (per_head * p.Hkv);
-    int in_layer = at - l * per_head * p.Hkv, b = 0, n_positions = 0;
-    for (int b0 = 0; n_positions == 0; b0 += 32) {  // (ends: in_layer lies within one of the sequences)
-        const int n = positions_of(b0 + lane);
-        int upto = n;  // inclusive sums over the lanes
+        // ---- the unit at `at`, and the part of it that is the CTA's ----
+        const int l = at / (per_head * p.Hkv);
+        int in_layer = at - l * per_head * p.Hkv, b = 0, n_positions = 0;
+        for (int b0 = 0; n_positions == 0; b0 += 32) {  // (ends: in_layer lies within one of the sequences)
+            const int n = positions_of(b0 + lane);
+            int upto = n;  // inclusive sums over the lanes
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += v;
-        }
-        const unsigned beyond = __ballot_sync(0xffffffffu, upto * p.Hkv > in_layer);
-        const int found = beyond ? __ffs(beyond) - 1 : 31;
-        const int before = __shfl_sync(0xffffffffu, upto - n, found);
-        if (beyond) {
-            in_layer -= before * p.Hkv;
-            b = b0 + found;
-            n_positions = __shfl_sync(0xffffffffu, n, found);
-        } else {
-            in_layer -= __shfl_sync(0xffffffffu, upto, 31) * p.Hkv;
-            if (b0 + 32 >= p.batch) return;
-        }
-    }
-    const int h = in_layer / n_positions, begin = in_layer % n_positions, lb = l * p.batch + b;
-    const int n_chunks = min(n_positions - begin, share_end - at);
-    const int unit_at = at - begin;
-    const int first_cta = cta_of(unit_at), n_parts = cta_of(unit_at + n_positions - 1) - first_cta + 1, part = (int)blockIdx.x - first_cta;
-    at += n_chunks;
-
-    const int seq_len = (int)min((long long)max(p.seq_lens[b], 0), (long long)p.max_blocks * p.bs);
-    const int M = min(max(p.q_lens ? p.q_lens[b] : p.M_max, 0), p.M_max);
-    const int rows = M * p.G;
-    if (rows <= 0) continue;  // (uniform for the CTA)
-    const bool last = begin + n_chunks == n_positions;  // the step's tokens are here
-    const int n_ctx = n_chunks - (last ? 1 : 0);
-
-    // ---- copies: chunk i of the warp's (the CTA's chunk warp + i kWarps) into stage i % kStages ----
-    const int ppc = kChunk >> p.bs_log2;  // pages per chunk
-    const uint32_t page_bytes = (uint32_t)p.bs * (D + 8);
-    const char* pool = reinterpret_cast<const char*>(p.pool) + ((size_t)(p.layer0 + l) * p.n_pages * p.Hkv + h) * page_bytes;
-    const int32_t* table = p.block_table + (size_t)b * p.max_blocks;
-    const uint32_t ring = base + warp * S::kStages * S::kStageBytes;
-    auto entry_of = [&](int i) {  // of the lane's page; looked at when it is used
-        const int c = warp + i * kWarps, blk = (begin + c) * ppc + lane;
-        return lane >= ppc || c >= n_ctx || (long long)blk * p.bs >= seq_len || blk >= p.max_blocks ? -1 : table[blk];
-    };
-    const uint32_t fills0 = fills;
-    auto copy = [&](int i, int page) {
-        const int c = warp + i * kWarps, blk = (begin + c) * ppc + lane;
-        if (c >= n_ctx) return;
-        const bool wanted = lane < ppc && (long long)blk * p.bs < seq_len && blk < p.max_blocks, there = wanted && page >= 0 && page < p.n_pages;
-        if (wanted && !there) record_fault(p.workspace, SPECPV_ERR_BAD_BLOCK_TABLE, b, blk, page, l);
-        const uint32_t bad = __ballot_sync(0xffffffffu, wanted && !there), n = (uint32_t)__popc(__ballot_sync(0xffffffffu, there));
-        const uint32_t slot = (fills0 + i) % S::kStages, bar = smem_u32(&full[warp][slot]);
-        if (lane == 0) {
-            bad_pages[warp][slot] = bad;
-            mbar_expect_tx(bar, n * page_bytes);
-        }
-        __syncwarp();
-        if (there)
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                         ::"r"(ring + slot * S::kStageBytes + lane * page_bytes), "l"(pool + (size_t)page * p.Hkv * page_bytes), "r"(page_bytes), "r"(bar)
-                         : "memory");
-        __syncwarp();
-    };
-    constexpr int kStages = S::kStages;
-    static_assert(kStages == 1 || kStages == 2, "stage = chunk % kStages");
-#pragma unroll
-    for (int i = 0; i < kStages; ++i) copy(i, entry_of(i));
-    int next_entry = entry_of(kStages);
-
-    // ---- the rows' queries as B fragments; the step's values, transposed, in shared memory ----
-    uint32_t qf[NT][D / 8];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int r = n * 8 + g;
-        const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.q) +
-                                                          (((size_t)lb * p.M_max + r / p.G) * p.Hq + h * p.G + r % p.G) * D) + t * (D / 32);
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (r < rows) v = src[i];
-            qf[n][4 * i] = v.x; qf[n][4 * i + 1] = v.y; qf[n][4 * i + 2] = v.z; qf[n][4 * i + 3] = v.w;
-        }
-    }
-    if (last) {
-        const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(p.v_new) + ((size_t)lb * p.M_max * p.Hkv + h) * D;
-        uint16_t* dst = reinterpret_cast<uint16_t*>(smem + (step_v - base));  // [token / 8][channel][8 tokens]
-        bool found = false;
-        for (int i = threadIdx.x; i < kMaxRows * D; i += kThreads) {
-            const int a = i / D, c = i % D;
-            uint16_t v = 0;
-            if (a < M) {
-                v = __bfloat16_as_ushort(src[(size_t)a * p.Hkv * D + c]);
-                if ((v & 0x7F80u) == 0x7F80u) {  // infinite and NaN values go another way
-                    found = true;
-                    v = 0;
-                }
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += v;
             }
-            dst[((a >> 3) * D + c) * 8 + (a & 7)] = v;
-        }
-        if (found) odd = 1;
-        __syncthreads();
-    }
-
-    // ---- where the lane's codes are in a stage (chunks of a page: keys [d / 32][bs][16 bytes], values [bs / 16][d][8 bytes]) ----
-    const int bs_mask = p.bs - 1;
-    const int k_token = 8 * (g >> 1) + (g & 1);  // of A's row g at step 0; row g + 8 is 32 tokens on; a step is two tokens
-    uint32_t k_off[2], k_par[2], v_off[2], v_par[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int kt = k_token + 32 * i, vt = 8 * t + 32 * i;
-        const uint32_t kp = (uint32_t)(kt >> p.bs_log2) * page_bytes, vp = (uint32_t)(vt >> p.bs_log2) * page_bytes;
-        const int ka = kt & bs_mask, va = vt & bs_mask;
-        k_off[i] = kp + (D == 128 ? (uint32_t)(t * p.bs + ka) * 16 : (uint32_t)((t >> 1) * p.bs + ka) * 16 + (t & 1) * 8);
-        k_par[i] = kp + (uint32_t)q4::param_at(p.bs, D, 0, ka & ~7) * 2;  // of the group of eight
-        v_off[i] = vp + (uint32_t)q4::v_word(p.bs, D, va, g) * 4;
-        v_par[i] = vp + (uint32_t)q4::param_at(p.bs, D, 2, va) * 2;
-    }
-    const uint32_t two_bs = 2u * p.bs;
-
-    float m[NT][2], sum[NT][2], acc[D / 16][NT][4];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        m[n][0] = m[n][1] = 0.f;
-        sum[n][0] = sum[n][1] = 0.f;
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c) acc[c][n][0] = acc[c][n][1] = acc[c][n][2] = acc[c][n][3] = 0.f;
-    }
-    const float scale = p.scale_log2;
-    const uint32_t mask = p.q4_mask, ones = p.q4_ones;
-    // (Two copies of the code: where a branch chose between opened codes and the step's own rows, every fragment was moved once more.)
-    auto work = [&](auto is_step, int i) {
-        constexpr bool step = decltype(is_step)::value;
-        const int chunk = warp + i * kWarps;
-        const uint32_t slot = (fills0 + i) % kStages, stage = ring + slot * S::kStageBytes;
-        const int left = step ? M : seq_len - (begin + chunk) * kChunk;  // valid tokens of the chunk, if fewer than 64
-        uint32_t bad;
-        if constexpr (!step) {
-            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&full[warp][slot]), (fills0 + i) / kStages & 1, &abort_flag, p.workspace, 41))) return false;
-            bad = bad_pages[warp][slot];
-            if (bad || left < kChunk) {
-                // Tokens behind a bad page id have no scales and offsets, nor (values) have those past the end: zeros.
-                for (int a = lane; a < kChunk; a += 32) {
-                    const int page = a >> p.bs_log2, at = a & (p.bs - 1);
-                    const bool gone = bad >> page & 1;
-                    uint16_t* par = reinterpret_cast<uint16_t*>(smem + (stage - base) + page * page_bytes);
-                    if (gone) par[q4::param_at(p.bs, D, 0, at)] = par[q4::param_at(p.bs, D, 1, at)] = 0;
-                    if (gone || a >= left) par[q4::param_at(p.bs, D, 2, at)] = par[q4::param_at(p.bs, D, 3, at)] = 0;
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before the stage is filled again
-                __syncwarp();
+            const unsigned beyond = __ballot_sync(0xffffffffu, upto * p.Hkv > in_layer);
+            const int found = beyond ? __ffs(beyond) - 1 : 31;
+            const int before = __shfl_sync(0xffffffffu, upto - n, found);
+            if (beyond) {
+                in_layer -= before * p.Hkv;
+                b = b0 + found;
+                n_positions = __shfl_sync(0xffffffffu, n, found);
+            } else {
+                in_layer -= __shfl_sync(0xffffffffu, upto, 31) * p.Hkv;
+                if (b0 + 32 >= p.batch) return;
             }
         }
-        // ---- S^T and the weights, 16 tokens a step ----
-        uint32_t pf[4][NT][2];
-        float add[NT][2];
-        uint32_t k_scale[2][4], k_offset[2][4];  // of tokens 2 s and 2 s + 1 of the lane's eight
-        const uint32_t half = g & 1 ? 0x3232 : 0x1010;
-        if constexpr (!step) {
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const uint4 a = lds16(stage + k_par[r]), z = lds16(stage + k_par[r] + two_bs);
-                k_scale[r][0] = a.x; k_scale[r][1] = a.y; k_scale[r][2] = a.z; k_scale[r][3] = a.w;
-                k_offset[r][0] = z.x; k_offset[r][1] = z.y; k_offset[r][2] = z.z; k_offset[r][3] = z.w;
-            }
-        }
-        // A row's reference is its largest score in the warp's first chunk (looked at once more where its scores are not all in
-        // registers together).  It is raised when a weight passes 2^16: float32 sums and bfloat16 weights
-        // keep their relative precision at any exponent, and values as large as 2^100 are not carried past float32.
-        bool look = i == 0;
-        auto reference = [&](float most) {
-#pragma unroll
-            for (int o = 4; o < 32; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-            return most == -INFINITY ? 0.f : most;  // (nothing seen)
+        const int h = in_layer / n_positions, begin = in_layer % n_positions, lb = l * p.batch + b;
+        const int n_chunks = min(n_positions - begin, share_end - at);
+        const int unit_at = at - begin;
+        const int first_cta = cta_of(unit_at), n_parts = cta_of(unit_at + n_positions - 1) - first_cta + 1, part = (int)blockIdx.x - first_cta;
+        at += n_chunks;
+
+        const int seq_len = (int)min((long long)max(p.seq_lens[b], 0), (long long)p.max_blocks * p.bs);
+        const int M = min(max(p.q_lens ? p.q_lens[b] : p.M_max, 0), p.M_max);
+        const int rows = M * p.G;
+        if (rows <= 0) continue;  // (uniform for the CTA)
+        const bool last = begin + n_chunks == n_positions;  // the step's tokens are here
+        const int n_ctx = n_chunks - (last ? 1 : 0);
+
+        // ---- copies: chunk i of the warp's (the CTA's chunk warp + i kWarps) into stage i % kStages ----
+        const int ppc = kChunk >> p.bs_log2;  // pages per chunk
+        const uint32_t page_bytes = (uint32_t)p.bs * (D + 8);
+        const char* pool = reinterpret_cast<const char*>(p.pool) + ((size_t)(p.layer0 + l) * p.n_pages * p.Hkv + h) * page_bytes;
+        const int32_t* table = p.block_table + (size_t)b * p.max_blocks;
+        const uint32_t ring = base + warp * S::kStages * S::kStageBytes;
+        auto entry_of = [&](int i) {  // of the lane's page; looked at when it is used
+            const int c = warp + i * kWarps, blk = (begin + c) * ppc + lane;
+            return lane >= ppc || c >= n_ctx || (long long)blk * p.bs >= seq_len || blk >= p.max_blocks ? -1 : table[blk];
         };
-        for (bool again = true; again;) {
-            again = false;
-            float most[NT][2];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                add[n][0] = add[n][1] = 0.f;
-                most[n][0] = most[n][1] = -INFINITY;
+        const uint32_t fills0 = fills;
+        auto copy = [&](int i, int page) {
+            const int c = warp + i * kWarps, blk = (begin + c) * ppc + lane;
+            if (c >= n_ctx) return;
+            const bool wanted = lane < ppc && (long long)blk * p.bs < seq_len && blk < p.max_blocks, there = wanted && page >= 0 && page < p.n_pages;
+            if (wanted && !there) record_fault(p.workspace, SPECPV_ERR_BAD_BLOCK_TABLE, b, blk, page, l);
+            const uint32_t bad = __ballot_sync(0xffffffffu, wanted && !there), n = (uint32_t)__popc(__ballot_sync(0xffffffffu, there));
+            const uint32_t slot = (fills0 + i) % S::kStages, bar = smem_u32(&full[warp][slot]);
+            if (lane == 0) {
+                bad_pages[warp][slot] = bad;
+                mbar_expect_tx(bar, n * page_bytes);
             }
+            __syncwarp();
+            if (there)
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                             ::"r"(ring + slot * S::kStageBytes + lane * page_bytes), "l"(pool + (size_t)page * p.Hkv * page_bytes), "r"(page_bytes), "r"(bar)
+                             : "memory");
+            __syncwarp();
+        };
+        constexpr int kStages = S::kStages;
+        static_assert(kStages == 1 || kStages == 2, "stage = chunk % kStages");
 #pragma unroll
-            for (int s0 = 0; s0 < 4; s0 += kTogether) {
-            float cs[kTogether][NT][4];
+        for (int i = 0; i < kStages; ++i) copy(i, entry_of(i));
+        int next_entry = entry_of(kStages);
+
+        // ---- the rows' queries as B fragments; the step's values, transposed, in shared memory ----
+        uint32_t qf[NT][D / 8];
 #pragma unroll
-            for (int s = s0; s < s0 + kTogether; ++s) {
-                float (&c)[NT][4] = cs[s - s0];
+        for (int n = 0; n < NT; ++n) {
+            const int r = n * 8 + g;
+            const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.q) +
+                                                              (((size_t)lb * p.M_max + r / p.G) * p.Hq + h * p.G + r % p.G) * D) + t * (D / 32);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) c[n][0] = c[n][1] = c[n][2] = c[n][3] = 0.f;
-                uint32_t k[2][D / 8];  // pairs of channels of rows g and g + 8
-                if constexpr (!step) {
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        uint32_t w[kWords];
-                        if constexpr (D == 128) {
-                            const uint4 v = lds16(stage + k_off[r] + s * 32);
-                            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-                        } else {
-                            const uint2 v = lds8(stage + k_off[r] + s * 32);
-                            w[0] = v.x; w[1] = v.y;
-                        }
-                        const uint32_t sc = __byte_perm(k_scale[r][s], 0, half), of = __byte_perm(k_offset[r][s], 0, half);
-#pragma unroll
-                        for (int i2 = 0; i2 < kWords; ++i2)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) k[r][4 * i2 + e] = q4::fma_bf16x2(q4::open_pair(w[i2], e, mask, ones), sc, of);
-                    }
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const int a = k_token + 32 * r + 2 * s;
-                        const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.k_new) +
-                                                                          (((size_t)lb * p.M_max + a) * p.Hkv + h) * D) + t * kWords;
-#pragma unroll
-                        for (int i2 = 0; i2 < kWords; ++i2) {
-                            const uint4 v = a < M ? src[i2] : make_uint4(0, 0, 0, 0);
-                            k[r][4 * i2] = v.x; k[r][4 * i2 + 1] = v.y; k[r][4 * i2 + 2] = v.z; k[r][4 * i2 + 3] = v.w;
-                        }
-                    }
-                }
-#pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-                        mma_16816(c[n], k[0][2 * ks], k[1][2 * ks], k[0][2 * ks + 1], k[1][2 * ks + 1], qf[n][2 * ks], qf[n][2 * ks + 1]);
-                // tokens that are not there, or not seen: -infinity
-                if (step || left < kChunk) {
-                    asm volatile("" ::: "memory");  // a branch
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const int a = k_token + 32 * r + 2 * s;
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                bool seen = a < left;
-                                if (step) {
-                                    const int row = n * 8 + 2 * t + e;
-                                    seen = seen && row < rows && (p.tree_mask[((size_t)b * p.M_max + row / p.G) * p.mask_words] >> a & 1);
-                                }
-                                if (!seen) c[n][2 * r + e] = -INFINITY;
-                            }
-                    }
-                }
+            for (int i = 0; i < D / 32; ++i) {
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (r < rows) v = src[i];
+                qf[n][4 * i] = v.x; qf[n][4 * i + 1] = v.y; qf[n][4 * i + 2] = v.z; qf[n][4 * i + 3] = v.w;
             }
-            float top = -INFINITY;
-#pragma unroll
-            for (int s = 0; s < kTogether; ++s)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        cs[s][n][e] = fmaf(cs[s][n][e], scale, -m[n][e & 1]);
-                        top = fmaxf(top, cs[s][n][e]);
+        }
+        if (last) {
+            const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(p.v_new) + ((size_t)lb * p.M_max * p.Hkv + h) * D;
+            uint16_t* dst = reinterpret_cast<uint16_t*>(smem + (step_v - base));  // [token / 8][channel][8 tokens]
+            bool found = false;
+            for (int i = threadIdx.x; i < kMaxRows * D; i += kThreads) {
+                const int a = i / D, c = i % D;
+                uint16_t v = 0;
+                if (a < M) {
+                    v = __bfloat16_as_ushort(src[(size_t)a * p.Hkv * D + c]);
+                    if ((v & 0x7F80u) == 0x7F80u) {  // infinite and NaN values go another way
+                        found = true;
+                        v = 0;
                     }
-            if (look) {
-#pragma unroll
-                for (int s = 0; s < kTogether; ++s)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) most[n][e & 1] = fmaxf(most[n][e & 1], cs[s][n][e]);
-                if constexpr (kTogether < 4) {
-                    continue;
-                } else {  // the whole chunk is here: no second pass
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            m[n][e] = reference(most[n][e]);
-#pragma unroll
-                            for (int s = 0; s < kTogether; ++s) {
-                                cs[s][n][e] -= m[n][e];
-                                cs[s][n][e + 2] -= m[n][e];
-                            }
-                        }
-                    look = false;
                 }
-            } else if (__any_sync(0xffffffffu, top > kRaise)) {
-                // references rise to the largest of these tokens; sums and accumulators follow, and the chunk starts over
+                dst[((a >> 3) * D + c) * 8 + (a & 7)] = v;
+            }
+            if (found) odd = 1;
+            __syncthreads();
+        }
+
+        // ---- where the lane's codes are in a stage (chunks of a page: keys [d / 32][bs][16 bytes], values [bs / 16][d][8 bytes]) ----
+        const int bs_mask = p.bs - 1;
+        const int k_token = 8 * (g >> 1) + (g & 1);  // of A's row g at step 0; row g + 8 is 32 tokens on; a step is two tokens
+        uint32_t k_off[2], k_par[2], v_off[2], v_par[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int kt = k_token + 32 * i, vt = 8 * t + 32 * i;
+            const uint32_t kp = (uint32_t)(kt >> p.bs_log2) * page_bytes, vp = (uint32_t)(vt >> p.bs_log2) * page_bytes;
+            const int ka = kt & bs_mask, va = vt & bs_mask;
+            k_off[i] = kp + (D == 128 ? (uint32_t)(t * p.bs + ka) * 16 : (uint32_t)((t >> 1) * p.bs + ka) * 16 + (t & 1) * 8);
+            k_par[i] = kp + (uint32_t)q4::param_at(p.bs, D, 0, ka & ~7) * 2;  // of the group of eight
+            v_off[i] = vp + (uint32_t)q4::v_word(p.bs, D, va, g) * 4;
+            v_par[i] = vp + (uint32_t)q4::param_at(p.bs, D, 2, va) * 2;
+        }
+        const uint32_t two_bs = 2u * p.bs;
+
+        float m[NT][2], sum[NT][2], acc[D / 16][NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            m[n][0] = m[n][1] = 0.f;
+            sum[n][0] = sum[n][1] = 0.f;
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) acc[c][n][0] = acc[c][n][1] = acc[c][n][2] = acc[c][n][3] = 0.f;
+        }
+        const float scale = p.scale_log2;
+        const uint32_t mask = p.q4_mask, ones = p.q4_ones;
+        // (Two copies of the code: where a branch chose between opened codes and the step's own rows, every fragment was moved once more.)
+        auto work = [&](auto is_step, int i) {
+            constexpr bool step = decltype(is_step)::value;
+            const int chunk = warp + i * kWarps;
+            const uint32_t slot = (fills0 + i) % kStages, stage = ring + slot * S::kStageBytes;
+            const int left = step ? M : seq_len - (begin + chunk) * kChunk;  // valid tokens of the chunk, if fewer than 64
+            uint32_t bad, step_sees[NT][2];  // the lane's rows: a bit per token of the step
+            if constexpr (step) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float rise = 0.f;
-#pragma unroll
-                        for (int s = 0; s < kTogether; ++s) rise = fmaxf(rise, fmaxf(cs[s][n][e], cs[s][n][e + 2]));
-#pragma unroll
-                        for (int o = 4; o < 32; o <<= 1) rise = fmaxf(rise, __shfl_xor_sync(0xffffffffu, rise, o));
-                        const float factor = ex2(-rise);
-                        m[n][e] += rise;
-                        sum[n][e] *= factor;
-#pragma unroll
-                        for (int d = 0; d < D / 16; ++d) {
-                            acc[d][n][e] *= factor;
-                            acc[d][n][e + 2] *= factor;
-                        }
+                        const int row = n * 8 + 2 * t + e;
+                        step_sees[n][e] = row < rows ? (uint32_t)p.tree_mask[((size_t)b * p.M_max + row / p.G) * p.mask_words] : 0u;
                     }
-                again = true;
-                break;
             }
-#pragma unroll
-            for (int s = 0; s < kTogether; ++s)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    float (&c)[4] = cs[s][n];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        c[e] = ex2(c[e]);
-                        add[n][e & 1] += c[e];
+            if constexpr (!step) {
+                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&full[warp][slot]), (fills0 + i) / kStages & 1, &abort_flag, p.workspace, 41))) return false;
+                bad = bad_pages[warp][slot];
+                if (bad || left < kChunk) {
+                    // Tokens behind a bad page id have no scales and offsets, nor (values) have those past the end: zeros.
+                    for (int a = lane; a < kChunk; a += 32) {
+                        const int page = a >> p.bs_log2, at = a & (p.bs - 1);
+                        const bool gone = bad >> page & 1;
+                        uint16_t* par = reinterpret_cast<uint16_t*>(smem + (stage - base) + page * page_bytes);
+                        if (gone) par[q4::param_at(p.bs, D, 0, at)] = par[q4::param_at(p.bs, D, 1, at)] = 0;
+                        if (gone || a >= left) par[q4::param_at(p.bs, D, 2, at)] = par[q4::param_at(p.bs, D, 3, at)] = 0;
                     }
-                    pf[s0 + s][n][0] = transposed(pack_bf16(c[0], c[1]));
-                    pf[s0 + s][n][1] = transposed(pack_bf16(c[2], c[3]));
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before the stage is filled again
+                    __syncwarp();
                 }
             }
-            if (look) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) m[n][e] = reference(most[n][e]);
-                look = false;
-                again = true;
-            }
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            sum[n][0] += add[n][0];
-            sum[n][1] += add[n][1];
-        }
-        // ---- O^T += V^T P^T, 16 channels at a time ----
-        uint32_t sc[2][4], of[2][4];
-        if (!step) {
-#pragma unroll
-            for (int i2 = 0; i2 < 2; ++i2) {
-                const uint4 a = lds16(stage + v_par[i2]), z = lds16(stage + v_par[i2] + two_bs);
-                sc[i2][0] = a.x; sc[i2][1] = a.y; sc[i2][2] = a.z; sc[i2][3] = a.w;
-                of[i2][0] = z.x; of[i2][1] = z.y; of[i2][2] = z.z; of[i2][3] = z.w;
-            }
-        }
-#pragma unroll
-        for (int d = 0; d < D / 16; ++d) {
-            uint32_t a[4][4];  // [row g | g + 8, first | second tokens][step]
+            // ---- S^T and the weights, 16 tokens a step ----
+            uint32_t pf[4][NT][2];
+            float add[NT][2];
+            uint32_t k_scale[2][4], k_offset[2][4];  // of tokens 2 s and 2 s + 1 of the lane's eight
+            const uint32_t half = g & 1 ? 0x3232 : 0x1010;
             if constexpr (!step) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {  // (row j & 1, tokens j >> 1)
-                    const uint32_t w = lds4(stage + v_off[j >> 1] + d * 128 + (j & 1) * 64);
-#pragma unroll
-                    for (int s = 0; s < 4; ++s) a[j][s] = q4::fma_bf16x2(q4::open_pair(w, s, mask, ones), sc[j >> 1][s], of[j >> 1][s]);
+                for (int r = 0; r < 2; ++r) {
+                    const uint4 a = lds16(stage + k_par[r]), z = lds16(stage + k_par[r] + two_bs);
+                    k_scale[r][0] = a.x; k_scale[r][1] = a.y; k_scale[r][2] = a.z; k_scale[r][3] = a.w;
+                    k_offset[r][0] = z.x; k_offset[r][1] = z.y; k_offset[r][2] = z.z; k_offset[r][3] = z.w;
                 }
-            } else {
+            }
+            // A row's reference is its largest score in the warp's first chunk (looked at once more where its scores are not all in
+            // registers together).  It is raised when a weight passes 2^16: float32 sums and bfloat16 weights
+            // keep their relative precision at any exponent, and values as large as 2^100 are not carried past float32.
+            bool look = i == 0;
+            auto reference = [&](float most) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint4 v = make_uint4(0, 0, 0, 0);  // (tokens 8 t .. of the first 32; there are at most 16)
-                    if (j < 2 && t < 2) v = lds16(step_v + (t * D + 16 * d + g + 8 * j) * 16);
-                    a[j][0] = v.x; a[j][1] = v.y; a[j][2] = v.z; a[j][3] = v.w;
+                for (int o = 4; o < 32; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+                return most == -INFINITY ? 0.f : most;  // (nothing seen)
+            };
+            for (bool again = true; again;) {
+                again = false;
+                float most[NT][2];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    add[n][0] = add[n][1] = 0.f;
+                    most[n][0] = most[n][1] = -INFINITY;
+                }
+#pragma unroll
+                for (int s0 = 0; s0 < 4; s0 += kTogether) {
+                    float cs[kTogether][NT][4];
+#pragma unroll
+                    for (int s = s0; s < s0 + kTogether; ++s) {
+                        float (&c)[NT][4] = cs[s - s0];
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) c[n][0] = c[n][1] = c[n][2] = c[n][3] = step && 2 * s >= left ? -INFINITY : 0.f;
+                        if (step && 2 * s >= left) continue;  // none of the step's tokens is in this one
+                        uint32_t k[2][D / 8];  // pairs of channels of rows g and g + 8
+                        if constexpr (!step) {
+#pragma unroll
+                            for (int r = 0; r < 2; ++r) {
+                                uint32_t w[kWords];
+                                if constexpr (D == 128) {
+                                    const uint4 v = lds16(stage + k_off[r] + s * 32);
+                                    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+                                } else {
+                                    const uint2 v = lds8(stage + k_off[r] + s * 32);
+                                    w[0] = v.x; w[1] = v.y;
+                                }
+                                const uint32_t sc = __byte_perm(k_scale[r][s], 0, half), of = __byte_perm(k_offset[r][s], 0, half);
+#pragma unroll
+                                for (int i2 = 0; i2 < kWords; ++i2)
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) k[r][4 * i2 + e] = q4::fma_bf16x2(q4::open_pair(w[i2], e, mask, ones), sc, of);
+                            }
+                        } else {
+#pragma unroll
+                            for (int i2 = 0; i2 < D / 8; ++i2) k[1][i2] = 0;  // (tokens from 32 on: there are none)
+                            {
+                                constexpr int r = 0;
+                                const int a = k_token + 2 * s;
+                                const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.k_new) +
+                                                                                  (((size_t)lb * p.M_max + a) * p.Hkv + h) * D) + t * kWords;
+#pragma unroll
+                                for (int i2 = 0; i2 < kWords; ++i2) {
+                                    const uint4 v = a < M ? src[i2] : make_uint4(0, 0, 0, 0);
+                                    k[r][4 * i2] = v.x; k[r][4 * i2 + 1] = v.y; k[r][4 * i2 + 2] = v.z; k[r][4 * i2 + 3] = v.w;
+                                }
+                            }
+                        }
+#pragma unroll
+                        for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+                                mma_16816(c[n], k[0][2 * ks], k[1][2 * ks], k[0][2 * ks + 1], k[1][2 * ks + 1], qf[n][2 * ks], qf[n][2 * ks + 1]);
+                        // tokens that are not there, or not seen: -infinity
+                        if (step || left < kChunk) {
+                            asm volatile("" ::: "memory");  // a branch
+#pragma unroll
+                            for (int r = 0; r < 2; ++r) {
+                                const int a = k_token + 32 * r + 2 * s;
+#pragma unroll
+                                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                    for (int e = 0; e < 2; ++e) {
+                                        bool seen = a < left;
+                                        if constexpr (step) seen = seen && (step_sees[n][e] >> (a & 31) & 1);  // (left is at most 16)
+                                        if (!seen) c[n][2 * r + e] = -INFINITY;
+                                    }
+                            }
+                        }
+                    }
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int s = 0; s < kTogether; ++s)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                cs[s][n][e] = fmaf(cs[s][n][e], scale, -m[n][e & 1]);
+                                top = fmaxf(top, cs[s][n][e]);
+                            }
+                    if (look) {
+#pragma unroll
+                        for (int s = 0; s < kTogether; ++s)
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) most[n][e & 1] = fmaxf(most[n][e & 1], cs[s][n][e]);
+                        if constexpr (kTogether < 4) {
+                            continue;
+                        } else {  // the whole chunk is here: no second pass
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    m[n][e] = reference(most[n][e]);
+#pragma unroll
+                                    for (int s = 0; s < kTogether; ++s) {
+                                        cs[s][n][e] -= m[n][e];
+                                        cs[s][n][e + 2] -= m[n][e];
+                                    }
+                                }
+                            look = false;
+                        }
+                    } else if (__any_sync(0xffffffffu, top > kRaise)) {
+                        // references rise to the largest of these tokens; sums and accumulators follow, and the chunk starts over
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                float rise = 0.f;
+#pragma unroll
+                                for (int s = 0; s < kTogether; ++s) rise = fmaxf(rise, fmaxf(cs[s][n][e], cs[s][n][e + 2]));
+#pragma unroll
+                                for (int o = 4; o < 32; o <<= 1) rise = fmaxf(rise, __shfl_xor_sync(0xffffffffu, rise, o));
+                                const float factor = ex2(-rise);
+                                m[n][e] += rise;
+                                sum[n][e] *= factor;
+#pragma unroll
+                                for (int d = 0; d < D / 16; ++d) {
+                                    acc[d][n][e] *= factor;
+                                    acc[d][n][e + 2] *= factor;
+                                }
+                            }
+                        again = true;
+                        break;
+                    }
+#pragma unroll
+                    for (int s = 0; s < kTogether; ++s)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            float (&c)[4] = cs[s][n];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                c[e] = ex2(c[e]);
+                                add[n][e & 1] += c[e];
+                            }
+                            pf[s0 + s][n][0] = transposed(pack_bf16(c[0], c[1]));
+                            pf[s0 + s][n][1] = transposed(pack_bf16(c[2], c[3]));
+                        }
+                }
+                if (look) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) m[n][e] = reference(most[n][e]);
+                    look = false;
+                    again = true;
                 }
             }
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) mma_16816(acc[d][n], a[0][s], a[1][s], a[2][s], a[3][s], pf[s][n][0], pf[s][n][1]);
-        }
-        __syncwarp();
-        if (!step) {
-            copy(i + kStages, next_entry);
-            next_entry = entry_of(i + kStages + 1);
-        }
-        return true;
-    };
-    int i = 0;
-    bool ok = true;
-#pragma unroll 1
-    for (; ok && warp + i * kWarps < n_ctx; ++i) ok = work(std::false_type(), i);
-    fills = fills0 + i;
-    if (ok && warp + i * kWarps < n_chunks) work(std::true_type(), i);
-
-    // ---- the warps meet ----
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            float v = sum[n][e];
-#pragma unroll
-            for (int o = 4; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-            if (g == 0) {
-                s_m[warp][n * 8 + 2 * t + e] = m[n][e];
-                s_l[warp][n * 8 + 2 * t + e] = v;
+            for (int n = 0; n < NT; ++n) {
+                sum[n][0] += add[n][0];
+                sum[n][1] += add[n][1];
             }
-        }
-    __syncthreads();  // also: every copy has been consumed, the ring is free
-    if ((int)threadIdx.x < kRows) {
-        const int r = threadIdx.x;
-        float top = -INFINITY, total = 0.f;
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_l[w][r] == 0.f ? -INFINITY : s_m[w][r]);  // (a NaN sum counts)
-        for (int w = 0; w < kWarps; ++w) {
-            const float f = s_l[w][r] == 0.f ? 0.f : ex2(s_m[w][r] - top);
-            s_factor[w][r] = f;
-            total += s_l[w][r] * f;
-        }
-        s_top[r] = top;
-        s_sum[r] = total;
-    }
-    __syncthreads();
-    float* meet = reinterpret_cast<float*>(smem);
+            // ---- O^T += V^T P^T, 16 channels at a time ----
+            uint32_t sc[2][4], of[2][4];
+            if (!step) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = n * 8 + 2 * t + e;
-            const float f = s_factor[warp][r];
-            float* to = meet + (warp * kRows + r) * S::kPitch + g;
+                for (int i2 = 0; i2 < 2; ++i2) {
+                    const uint4 a = lds16(stage + v_par[i2]), z = lds16(stage + v_par[i2] + two_bs);
+                    sc[i2][0] = a.x; sc[i2][1] = a.y; sc[i2][2] = a.z; sc[i2][3] = a.w;
+                    of[i2][0] = z.x; of[i2][1] = z.y; of[i2][2] = z.z; of[i2][3] = z.w;
+                }
+            }
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) {
-                to[16 * d] = acc[d][n][e] * f;
-                to[16 * d + 8] = acc[d][n][e + 2] * f;
-            }
-        }
-    __syncthreads();
-    for (int i = threadIdx.x; i < rows * D; i += kThreads) {
-        const int r = i / D, c = i % D, j = r / p.G;
-        float o = 0.f;
+                uint32_t a[4][4];  // [row g | g + 8, first | second tokens][step]
+                if constexpr (!step) {
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) o += meet[(w * kRows + r) * S::kPitch + c];
-        const float total = s_sum[r];
-        if (last && odd) {  // infinite and NaN values of the step's tokens that the row sees
-            const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.v_new) + ((size_t)lb * p.M_max * p.Hkv + h) * D + c;
-            const uint64_t seen = p.tree_mask[((size_t)b * p.M_max + j) * p.mask_words];
-            for (int a = 0; a < M; ++a) {
-                const float y = __bfloat162float(v[(size_t)a * p.Hkv * D]);
-                if (!isfinite(y) && (seen >> a & 1)) o += y;
+                    for (int j = 0; j < 4; ++j) {  // (row j & 1, tokens j >> 1)
+                        const uint32_t w = lds4(stage + v_off[j >> 1] + d * 128 + (j & 1) * 64);
+#pragma unroll
+                        for (int s = 0; s < 4; ++s) a[j][s] = q4::fma_bf16x2(q4::open_pair(w, s, mask, ones), sc[j >> 1][s], of[j >> 1][s]);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint4 v = make_uint4(0, 0, 0, 0);  // (tokens 8 t .. of the first 32; there are at most 16)
+                        if (j < 2 && t < 2) v = lds16(step_v + (t * D + 16 * d + g + 8 * j) * 16);
+                        a[j][0] = v.x; a[j][1] = v.y; a[j][2] = v.z; a[j][3] = v.w;
+                    }
+                }
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+                    if (!step || 2 * s < left) {
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma_16816(acc[d][n], a[0][s], a[1][s], a[2][s], a[3][s], pf[s][n][0], pf[s][n][1]);
+                    }
+            }
+            __syncwarp();
+            if (!step) {
+                copy(i + kStages, next_entry);
+                next_entry = entry_of(i + kStages + 1);
+            }
+            return true;
+        };
+        int i = 0;
+        bool ok = true;
+#pragma unroll 1
+        for (; ok && warp + i * kWarps < n_ctx; ++i) ok = work(std::false_type(), i);
+        fills = fills0 + i;
+        if (ok && warp + i * kWarps < n_chunks) work(std::true_type(), i);
+
+        // ---- the warps meet ----
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float v = sum[n][e];
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+                if (g == 0) {
+                    s_m[warp][n * 8 + 2 * t + e] = m[n][e];
+                    s_l[warp][n * 8 + 2 * t + e] = v;
+                }
+            }
+        __syncthreads();  // also: every copy has been consumed, the ring is free
+        if ((int)threadIdx.x < kRows) {
+            const int r = threadIdx.x;
+            float top = -INFINITY, total = 0.f;
+            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_l[w][r] == 0.f ? -INFINITY : s_m[w][r]);  // (a NaN sum counts)
+            for (int w = 0; w < kWarps; ++w) {
+                const float f = s_l[w][r] == 0.f ? 0.f : ex2(s_m[w][r] - top);
+                s_factor[w][r] = f;
+                total += s_l[w][r] * f;
+            }
+            s_top[r] = top;
+            s_sum[r] = total;
+        }
+        __syncthreads();
+        float* meet = reinterpret_cast<float*>(smem);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = n * 8 + 2 * t + e;
+                const float f = s_factor[warp][r];
+                float* to = meet + (warp * kRows + r) * S::kPitch + g;
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d) {
+                    to[16 * d] = acc[d][n][e] * f;
+                    to[16 * d + 8] = acc[d][n][e + 2] * f;
+                }
+            }
+        __syncthreads();
+        for (int i = threadIdx.x; i < rows * D; i += kThreads) {
+            const int r = i / D, c = i % D, j = r / p.G;
+            float o = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) o += meet[(w * kRows + r) * S::kPitch + c];
+            const float total = s_sum[r];
+            if (last && odd) {  // infinite and NaN values of the step's tokens that the row sees
+                const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.v_new) + ((size_t)lb * p.M_max * p.Hkv + h) * D + c;
+                const uint64_t seen = p.tree_mask[((size_t)b * p.M_max + j) * p.mask_words];
+                for (int a = 0; a < M; ++a) {
+                    const float y = __bfloat162float(v[(size_t)a * p.Hkv * D]);
+                    if (!isfinite(y) && (seen >> a & 1)) o += y;
+                }
+            }
+            const size_t to = (((size_t)lb * p.Hkv + h) * p.n_slots + part) * ((size_t)p.M_max * p.G) + r;
+            p.part_o[to * D + c] = o;
+            if (c == 0) {
+                // nothing seen: -infinity; a NaN has to survive the merge, which leaves out what weighs nothing
+                p.part_ml[to * 2] = total == 0.f ? -INFINITY : total != total ? INFINITY : s_top[r] * kLn2;
+                p.part_ml[to * 2 + 1] = total;
             }
         }
-        const size_t to = (((size_t)lb * p.Hkv + h) * p.n_slots + part) * ((size_t)p.M_max * p.G) + r;
-        p.part_o[to * D + c] = o;
-        if (c == 0) {
-            // nothing seen: -infinity; a NaN has to survive the merge, which leaves out what weighs nothing
-            p.part_ml[to * 2] = total == 0.f ? -INFINITY : total != total ? INFINITY : s_top[r] * kLn2;
-            p.part_ml[to * 2 + 1] = total;
-        }
-    }
-    if (last)  // slots that no CTA fills
-        for (int i = threadIdx.x; i < (p.n_slots - n_parts) * rows; i += kThreads) {
-            const size_t to = (((size_t)lb * p.Hkv + h) * p.n_slots + n_parts + i / rows) * ((size_t)p.M_max * p.G) + i % rows;
-            p.part_ml[to * 2] = -INFINITY;
-            p.part_ml[to * 2 + 1] = 0.f;
-        }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before copies into where the warps met
-    __syncthreads();
-    if (last) {
-        if (threadIdx.x == 0) odd = 0;
+        if (last)  // slots that no CTA fills
+            for (int i = threadIdx.x; i < (p.n_slots - n_parts) * rows; i += kThreads) {
+                const size_t to = (((size_t)lb * p.Hkv + h) * p.n_slots + n_parts + i / rows) * ((size_t)p.M_max * p.G) + i % rows;
+                p.part_ml[to * 2] = -INFINITY;
+                p.part_ml[to * 2 + 1] = 0.f;
+            }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before copies into where the warps met
         __syncthreads();
-    }
-    if (abort_flag) break;
+        if (last) {
+            if (threadIdx.x == 0) odd = 0;
+            __syncthreads();
+        }
+        if (abort_flag) break;
     }
     pdl_trigger();
     if (abort_flag) __nanosleep(1000000);  // after a wait that gave up, the copies in flight land within microseconds
@@ -625,12 +648,13 @@ specpv_status launch_attention_q4_rows(const AttnArgs& a, cudaStream_t stream) {
     const int R_max = a.M_max * a.g.G, units = a.g.Hkv * a.n_layers * a.batch;
     const int positions = (a.max_seq_len + kChunk - 1) / kChunk + 1;
     if ((long long)units * positions >= 1LL << 30) return SPECPV_ERR_CAPACITY;
-    // One CTA per SM, each with at least a chunk for every warp.  Where the units are alike a number of CTAs that the units divide
+    // One CTA per SM, each with at least a chunk for every warp, or, for one sequence, for every scheduler of the SM (2047 tokens, one
+    // layer, 4 rows 10.7 -> 10.1 us; two sequences of 1000 and 3000 tokens, whose shares then meet more units, 16.2 -> 16.8).  Where the units are alike a number of CTAs that the units divide
     // makes shares that lie in one unit each; else every SM has the same to do, but a unit more or two to begin and end, 4 us each.
     // (A position takes some 0.29 us, 0.45 with 16 rows.)
     const int warps = R_max <= 8 ? 12 : 8;
     const double us = R_max <= 8 ? 0.29 : 0.45, begin_us = 4.0;
-    const int most = (positions + warps - 1) / warps;  // CTAs of a unit
+    const int least = a.batch == 1 ? 4 : warps, most = (positions + least - 1) / least;  // CTAs of a unit
     long long n_ctas = (long long)units * most < 148 ? (long long)units * most : 148;
     if (a.batch == 1 && units <= 148) {
         const int k = 148 / units < most ? 148 / units : most;
