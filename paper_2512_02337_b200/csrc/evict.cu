@@ -2,6 +2,8 @@
 // tokens with the smallest accounts, after which the others close up.
 #include <math.h>
 
+#include <type_traits>
+
 #include "aux_kernels.cuh"
 #include "tc_common.cuh"
 
@@ -14,12 +16,16 @@ namespace {
 // tokens t that row i sees.  The keys are read once, at the rate of the memory (that is the bound), straight into the registers that
 // the warp-wide matrix instruction takes them from: a warp owns 16 tokens at a time, S^T [16 tokens x 8 rows] = K Q^T.  The sum over
 // channels may be taken in any order, so lane (g, t) keeps the 16 bytes at 16 (4 j + t) of tokens g and g + 8 as they come.  The
-// rows' queries wait in shared memory in the same order, 16 bytes a lane.  float32: both factors as two terms of 11 bits, three
-// products (m16n8k8), which leaves 2^-21 of a product.  A token's sum over the rows is formed in a fixed order: the same at every run.
+// rows' queries wait in shared memory in the same order, 16 bytes a lane.  (98309 tokens x 8 heads x 12 layers, 28 rows: 416 us, 92 % of
+// the copy rate; 510 with one chain of products per row tile, keys moved from buffer to buffer and divisions by the page size.)
+// float32: both factors as two terms of 11 bits, three products (m16n8k8), which leaves 2^-21 of a product; bound by forming the
+// terms and by the products (4261 tokens x 8 heads x 8 layers, 20 rows 74 us, 21 for its bytes; with terms formed per row tile and every
+// element tested for infinity 145).  A token's sum over the rows is formed in a fixed order: the same at every run.
 // ---------------------------------------------------------------------------------------------
 constexpr int kAccWarps = 8;
 constexpr int kAccTokens = 16;      // of a warp at a time
 constexpr int kAccPassRows = 128;   // rows per launch; more rows take several
+constexpr int kSharers = 3;         // row tiles that share a tile's terms (float32)
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -31,18 +37,21 @@ __device__ __forceinline__ void mma_tf32(float (&c)[4], uint32_t a0, uint32_t a1
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// x as two terms of 11 bits.  An infinity or NaN is the first alone, and `finite`, what the other factor's second term meets, is then 0:
-// its products are those with the other's first term, which has the sign and is zero only where the factor is.
-__device__ __forceinline__ void two_terms(uint32_t x, uint32_t& hi, uint32_t& finite, uint32_t& lo) {
+__device__ __forceinline__ bool is_odd(uint32_t x) { return (x & 0x7F800000u) == 0x7F800000u; }  // infinite or NaN
+// x as two terms of 11 bits.  With kCareful an infinity or NaN is the first alone, and what the other factor's second term meets is
+// then 0 (met_by_rest): its products are those with the other's first term, which has the sign and is zero only where the factor is.
+template <bool kCareful>
+__device__ __forceinline__ void two_terms(uint32_t x, uint32_t& hi, uint32_t& lo) {
     asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(__uint_as_float(x)));
     const float rest = __uint_as_float(x) - __uint_as_float(hi);
     asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(lo) : "f"(rest));
-    finite = hi;
-    if ((x & 0x7F800000u) == 0x7F800000u) {
+    if (kCareful && is_odd(x)) {
         hi = x;
-        finite = lo = 0;
+        lo = 0;
     }
 }
+template <bool kCareful>
+__device__ __forceinline__ uint32_t met_by_rest(uint32_t hi) { return kCareful && is_odd(hi) ? 0u : hi; }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulateParams p) {
@@ -58,12 +67,15 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
     const int tile0 = blockIdx.x * p.tiles_per_cta, tile1 = min(tile0 + p.tiles_per_cta, n_tiles);
     const int rows = min(p.row1, n * p.G) - p.row0, row_tiles = (rows + 7) / 8;
     if (tile0 >= tile1 || rows <= 0) return;
-    uint4* s_q = reinterpret_cast<uint4*>(acc_smem);  // [row tile][piece][lane]
-    float* s_lse = reinterpret_cast<float*>(s_q + row_tiles * kPieces * 32);  // [row], log2
+    constexpr int kTerms = kF32 ? 2 : 1;
+    uint4* s_q = reinterpret_cast<uint4*>(acc_smem);  // [term][row tile][piece][lane]
+    const int term_stride = row_tiles * kPieces * 32;
+    float* s_lse = reinterpret_cast<float*>(s_q + kTerms * term_stride);  // [row], log2
     int* s_end = reinterpret_cast<int*>(s_lse + row_tiles * 8);  // tokens that the row sees: none, if it adds nothing
-    __shared__ uint32_t s_idle;                               // bit per row tile: such rows are among it
+    __shared__ uint32_t s_idle;  // bit per row tile: such rows are among it
+    __shared__ int s_odd;        // a query's element is infinite or NaN (float32)
     static_assert(kAccPassRows / 8 <= 32, "a bit per row tile");
-    if (threadIdx.x == 0) s_idle = 0;
+    if (threadIdx.x == 0) s_idle = s_odd = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < row_tiles * 8; i += 32 * kAccWarps) {
         const int r = p.row0 + i, a = r / p.G;
@@ -89,8 +101,19 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
 #pragma unroll
         for (int j = 0; j < kPieces; ++j)
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-                s_q[((i >> 3) * kPieces + j) * 32 + (i & 7) * 4 + x] = row < 0 ? make_uint4(0, 0, 0, 0) : src[j * 4 + x];
+            for (int x = 0; x < 4; ++x) {
+                uint4 v = row < 0 ? make_uint4(0, 0, 0, 0) : src[j * 4 + x], rest;
+                uint4* to = s_q + ((i >> 3) * kPieces + j) * 32 + (i & 7) * 4 + x;
+                if constexpr (kF32) {
+                    if (is_odd(v.x) || is_odd(v.y) || is_odd(v.z) || is_odd(v.w)) s_odd = 1;
+                    two_terms<true>(v.x, v.x, rest.x);
+                    two_terms<true>(v.y, v.y, rest.y);
+                    two_terms<true>(v.z, v.z, rest.z);
+                    two_terms<true>(v.w, v.w, rest.w);
+                    to[term_stride] = rest;
+                }
+                *to = v;
+            }
     }
     __syncthreads();
     const uint32_t idle = s_idle;
@@ -129,35 +152,7 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
         entry = entry_of(tile + 2 * kAccWarps);
         const bool all_seen = (tile + 1) * kAccTokens <= seq_len - n;
         float sum[2] = {0.f, 0.f};
-#pragma unroll 1
-        for (int rt = 0; rt < row_tiles; ++rt) {
-            float c[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};  // two chains of products
-#pragma unroll
-            for (int j = 0; j < kPieces; ++j) {
-                const uint4 q = s_q[(rt * kPieces + j) * 32 + lane];
-                const uint4 k0 = now[0][j], k1 = now[1][j];
-                if constexpr (!kF32) {
-                    mma_bf16(c, k0.x, k1.x, k0.y, k1.y, q.x, q.y);
-                    mma_bf16(c1, k0.z, k1.z, k0.w, k1.w, q.z, q.w);
-                } else {
-                    const uint32_t kw[2][4] = {{k0.x, k0.y, k0.z, k0.w}, {k1.x, k1.y, k1.z, k1.w}}, qw[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-                    for (int x = 0; x < 4; x += 2) {
-                        uint32_t ah[4], af[4], al[4], bh[2], bf[2], bl[2];
-                        two_terms(kw[0][x], ah[0], af[0], al[0]);
-                        two_terms(kw[1][x], ah[1], af[1], al[1]);
-                        two_terms(kw[0][x + 1], ah[2], af[2], al[2]);
-                        two_terms(kw[1][x + 1], ah[3], af[3], al[3]);
-                        two_terms(qw[x], bh[0], bf[0], bl[0]);
-                        two_terms(qw[x + 1], bh[1], bf[1], bl[1]);
-                        mma_tf32(c1, al[0], al[1], al[2], al[3], bf[0], bf[1]);
-                        mma_tf32(c1, af[0], af[1], af[2], af[3], bl[0], bl[1]);
-                        mma_tf32(c, ah[0], ah[1], ah[2], ah[3], bh[0], bh[1]);
-                    }
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) c[e] += c1[e];
+        auto weigh = [&](int rt, const float (&c)[4]) {
             const float2 lse = *reinterpret_cast<const float2*>(s_lse + rt * 8 + 2 * t);
             float w[4] = {tc::ex2(fmaf(c[0], scale, -lse.x)), tc::ex2(fmaf(c[1], scale, -lse.y)), tc::ex2(fmaf(c[2], scale, -lse.x)),
                           tc::ex2(fmaf(c[3], scale, -lse.y))};
@@ -170,6 +165,75 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
             }
             sum[0] += w[0] + w[1];
             sum[1] += w[2] + w[3];
+        };
+        if constexpr (!kF32) {
+#pragma unroll 1
+            for (int rt = 0; rt < row_tiles; ++rt) {
+                float c[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};  // two chains of products
+#pragma unroll
+                for (int j = 0; j < kPieces; ++j) {
+                    const uint4 q = s_q[(rt * kPieces + j) * 32 + lane];
+                    mma_bf16(c, now[0][j].x, now[1][j].x, now[0][j].y, now[1][j].y, q.x, q.y);
+                    mma_bf16(c1, now[0][j].z, now[1][j].z, now[0][j].w, now[1][j].w, q.z, q.w);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) c[e] += c1[e];
+                weigh(rt, c);
+            }
+        } else {
+            auto products = [&](auto careful) {
+                constexpr bool kCareful = decltype(careful)::value;
+#pragma unroll 1
+                for (int rt0 = 0; rt0 < row_tiles; rt0 += kSharers) {  // the keys' terms are formed once for these
+                    float c[kSharers][4], c1[kSharers][4];
+#pragma unroll
+                    for (int u = 0; u < kSharers; ++u)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) c[u][e] = c1[u][e] = 0.f;
+#pragma unroll
+                    for (int j = 0; j < kPieces; ++j) {
+                        const uint32_t k0[4] = {now[0][j].x, now[0][j].y, now[0][j].z, now[0][j].w}, k1[4] = {now[1][j].x, now[1][j].y, now[1][j].z, now[1][j].w};
+                        uint32_t hi[2][4], rest[2][4], met[2][4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            two_terms<kCareful>(k0[x], hi[0][x], rest[0][x]);
+                            two_terms<kCareful>(k1[x], hi[1][x], rest[1][x]);
+                            met[0][x] = met_by_rest<kCareful>(hi[0][x]);
+                            met[1][x] = met_by_rest<kCareful>(hi[1][x]);
+                        }
+#pragma unroll
+                        for (int u = 0; u < kSharers; ++u) {
+                            if (rt0 + u >= row_tiles) break;
+                            const uint4* at = s_q + ((rt0 + u) * kPieces + j) * 32 + lane;
+                            const uint4 qh = at[0], ql = at[term_stride];
+                            const uint4 qm = make_uint4(met_by_rest<kCareful>(qh.x), met_by_rest<kCareful>(qh.y), met_by_rest<kCareful>(qh.z), met_by_rest<kCareful>(qh.w));
+                            mma_tf32(c1[u], rest[0][0], rest[1][0], rest[0][1], rest[1][1], qm.x, qm.y);
+                            mma_tf32(c[u], hi[0][0], hi[1][0], hi[0][1], hi[1][1], qh.x, qh.y);
+                            mma_tf32(c1[u], met[0][0], met[1][0], met[0][1], met[1][1], ql.x, ql.y);
+                            mma_tf32(c[u], hi[0][2], hi[1][2], hi[0][3], hi[1][3], qh.z, qh.w);
+                            mma_tf32(c1[u], rest[0][2], rest[1][2], rest[0][3], rest[1][3], qm.z, qm.w);
+                            mma_tf32(c1[u], met[0][2], met[1][2], met[0][3], met[1][3], ql.z, ql.w);
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < kSharers; ++u) {
+                        if (rt0 + u >= row_tiles) break;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) c[u][e] += c1[u][e];
+                        weigh(rt0 + u, c[u]);
+                    }
+                }
+            };
+            float z = 0.f;  // NaN if one of the keys' elements is infinite or NaN
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+                    z = fmaf(__uint_as_float(now[r][j].x), 0.f, fmaf(__uint_as_float(now[r][j].y), 0.f, fmaf(__uint_as_float(now[r][j].z), 0.f, fmaf(__uint_as_float(now[r][j].w), 0.f, z))));
+            if (__any_sync(0xffffffffu, z != z) || s_odd)
+                products(std::true_type());
+            else
+                products(std::false_type());
         }
 #pragma unroll
         for (int o = 1; o < 4; o <<= 1) {
@@ -194,7 +258,8 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
 // be read, because place j, as a source, belongs to a rank <= j.  For the same reason the next round's rows are requested before this
 // one's are written; where they are is known by then: one thread per row has asked for its index three rounds ahead and for the
 // table entries two ahead, so that no request waits for another.  Rows that stay are neither read nor written.  Bound by memory: every
-// moved row is read and written once.  grid = (cluster x 3 KV heads, layers x seqs).
+// moved row is read and written once (4096 of 4352 tokens, 8 heads x 32 layers: 222 us with the selection, 0.74 of the copy rate; with
+// each round's look-ups behind the round before 436).  grid = (cluster x 3 KV heads, layers x seqs).
 // ---------------------------------------------------------------------------------------------
 constexpr int kCloseThreads = 256;
 constexpr int kCloseLoads = 8;  // 16-byte loads in flight per thread and round
@@ -330,7 +395,7 @@ __global__ void __launch_bounds__(kLensThreads) evict_lens_kernel(EvictParams p)
 template <typename T, int D>
 static specpv_status launch_accumulate_typed(AccumulateParams p, int n_layers, int max_seq_len, cudaStream_t stream) {
     // Tiles per warp: the waves of CTAs, two on an SM, times what one takes, of which a start is about two and a half tiles (32 layers x 8
-    // heads x 4261 tokens, 20 rows: 58 us with 14 tiles per warp, kNowUs with the 17 chosen).
+    // heads x 4261 tokens, 20 rows: 73 us with 14 tiles per warp, 66 with the 17 chosen).
     const long long tiles = (max_seq_len + kAccTokens - 1) / kAccTokens, heads = (long long)p.Hkv * n_layers * p.batch;
     int per_warp = 1;
     double best = 1e300;
@@ -349,8 +414,9 @@ static specpv_status launch_accumulate_typed(AccumulateParams p, int n_layers, i
     for (p.row0 = 0; p.row0 < all_rows; p.row0 += kAccPassRows) {
         p.row1 = p.row0 + kAccPassRows;
         const int row_tiles = ((all_rows < p.row1 ? all_rows : p.row1) - p.row0 + 7) / 8;
-        const size_t smem = (size_t)row_tiles * 8 * (D * sizeof(T) + 8);
-        if (!tc::set_smem_limit_once(reinterpret_cast<const void*>(accumulate_kernel<T, D>), kAccPassRows * (D * (int)sizeof(T) + 8))) return SPECPV_ERR_CUDA;
+        constexpr int kRowBytes = D * (int)sizeof(T) * (sizeof(T) == 4 ? 2 : 1) + 8;
+        const size_t smem = (size_t)row_tiles * 8 * kRowBytes;
+        if (!tc::set_smem_limit_once(reinterpret_cast<const void*>(accumulate_kernel<T, D>), kAccPassRows * kRowBytes)) return SPECPV_ERR_CUDA;
         SPECPV_LAUNCH((accumulate_kernel<T, D>), grid, 32 * kAccWarps, smem, stream, p);
     }
     return SPECPV_OK;
