@@ -238,6 +238,12 @@ def test_eviction_from_long_lists(n, keep):
     run_evict("bf16", 2, 64, 64, [n], keep, 4, 32, layers=1, seed=n)
 
 
+@pytest.mark.parametrize("n,keep,shared", [(24001, 8192, 0), (24001, 23000, 1), (70001, 5000, 0), (70001, 69000, 1)])
+def test_eviction_from_lists_past_the_registers(n, keep, shared):
+    run_evict("bf16", 2, 64, 64, [n, 20000], keep, 32, 100, layers=1, seed=n, shared=shared)
+    run_evict("bf16", 1, 64, 64, [n], keep, 0, 0, layers=1, shared=shared, change=lambda acc: acc.fill_(2.0))
+
+
 def test_eviction_of_many_units_and_layers():
     run_evict("bf16", 8, 64, 16, [200, 150], 128, 4, 16, layers=12)
     run_evict("bf16", 3, 64, 16, [200, 150], 128, 4, 16, layers=2, shared=1)
