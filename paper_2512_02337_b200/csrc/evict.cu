@@ -24,7 +24,6 @@ namespace {
 // element tested for infinity 145).  A token's sum over the rows is formed in a fixed order: the same at every run.
 // ---------------------------------------------------------------------------------------------
 constexpr int kAccWarps = 8;
-constexpr float kLog2e = 1.4426950408889634f, kLog2eRest = (float)(1.4426950408889634 - (double)kLog2e);
 constexpr int kAccTokens = 16;      // of a warp at a time
 constexpr int kAccPassRows = 128;   // rows per launch; more rows take several
 constexpr int kSharers = 3;         // row tiles that share a tile's terms (float32)
@@ -72,8 +71,8 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
     constexpr int kTerms = kF32 ? 2 : 1;
     uint4* s_q = reinterpret_cast<uint4*>(acc_smem);  // [term][row tile][piece][lane]
     const int term_stride = row_tiles * kPieces * 32;
-    float* s_lse = reinterpret_cast<float*>(s_q + kTerms * term_stride);  // [row], log2; float32: [term][row]
-    int* s_end = reinterpret_cast<int*>(s_lse + row_tiles * 8 * kTerms);  // tokens that the row sees: none, if it adds nothing
+    float* s_lse = reinterpret_cast<float*>(s_q + kTerms * term_stride);  // [row], in the unit of the products
+    int* s_end = reinterpret_cast<int*>(s_lse + row_tiles * 8);  // tokens that the row sees: none, if it adds nothing
     __shared__ uint32_t s_idle;  // bit per row tile: such rows are among it
     __shared__ int s_odd;        // a query's element is infinite or NaN (float32)
     static_assert(kAccPassRows / 8 <= 32, "a bit per row tile");
@@ -81,7 +80,7 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
     __syncthreads();
     for (int i = threadIdx.x; i < row_tiles * 8; i += 32 * kAccWarps) {
         const int r = p.row0 + i, a = r / p.G;
-        float lse = 0.f, lost = 0.f;
+        float lse = 0.f;
         int row = -1, end = -1;
         if (i < rows) {
             row = p.accepted ? p.accepted[(size_t)b * p.A_max + a] : a;
@@ -91,15 +90,13 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
             } else {
                 const float natural = p.lse[((size_t)lb * p.M_max + row) * p.Hq + h * p.G + r % p.G];
                 if (natural != -INFINITY) {
-                    lse = natural * kLog2e;
-                    if (isfinite(lse)) lost = fmaf(natural, kLog2e, -lse) + natural * kLog2eRest;
+                    lse = natural / p.scale;
                     end = seq_len - n + a + 1;
                 }
             }
         }
         if (end < 0) atomicOr(&s_idle, 1u << (i >> 3));
         s_lse[i] = lse;
-        if constexpr (kF32) s_lse[row_tiles * 8 + i] = lost;
         s_end[i] = end;
         const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.q) + (((size_t)lb * p.M_max + max(row, 0)) * p.Hq + h * p.G + r % p.G) * D);
 #pragma unroll
@@ -125,7 +122,7 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
     const size_t page_stride = (size_t)p.Hkv * p.bs * (D * sizeof(T) / 16);
     const int32_t* table = p.block_table + (size_t)b * p.max_blocks;
     float* acc = p.acc + (((size_t)(p.layer0 + l) * p.batch + b) * p.Hkv + h) * (size_t)p.max_blocks * p.bs;
-    const float scale = p.scale * kLog2e, scale_rest = fmaf(p.scale, kLog2e, -scale) + p.scale * kLog2eRest;
+    const float scale = p.scale * 1.4426950408889634f;
     // tiles of 16 tokens divide a page (of 16, 32 or 64): page and place by shifts
     auto entry_of = [&](int tile) { return tile < tile1 ? table[tile >> p.tiles_log2] : -1; };
     auto fetch = [&](int tile, int page, uint4 (&x)[2][kPieces]) {  // keys of tokens g and g + 8; whether they are there
@@ -158,16 +155,8 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
         float sum[2] = {0.f, 0.f};
         auto weigh = [&](int rt, const float (&c)[4]) {
             const float2 lse = *reinterpret_cast<const float2*>(s_lse + rt * 8 + 2 * t);
-            float w[4] = {fmaf(c[0], scale, -lse.x), fmaf(c[1], scale, -lse.y), fmaf(c[2], scale, -lse.x), fmaf(c[3], scale, -lse.y)};
-            if constexpr (kF32) {  // what scale and lse lost when they were brought to base 2
-                const float2 lost = *reinterpret_cast<const float2*>(s_lse + (row_tiles + rt) * 8 + 2 * t);
-                w[0] += fmaf(c[0], scale_rest, -lost.x);
-                w[1] += fmaf(c[1], scale_rest, -lost.y);
-                w[2] += fmaf(c[2], scale_rest, -lost.x);
-                w[3] += fmaf(c[3], scale_rest, -lost.y);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = tc::ex2(w[e]);
+            // the difference first: where a weight counts it is small, and so then is what the factor's rounding takes from it
+            float w[4] = {tc::ex2((c[0] - lse.x) * scale), tc::ex2((c[1] - lse.y) * scale), tc::ex2((c[2] - lse.x) * scale), tc::ex2((c[3] - lse.y) * scale)};
             if (!all_seen || (idle >> rt & 1)) {  // (by choice, not by a weight of 0: the key may be infinite)
                 const int2 end = *reinterpret_cast<const int2*>(s_end + rt * 8 + 2 * t);
                 if (token >= end.x) w[0] = 0.f;
@@ -429,7 +418,7 @@ static specpv_status launch_accumulate_typed(AccumulateParams p, int n_layers, i
     for (p.row0 = 0; p.row0 < all_rows; p.row0 += kAccPassRows) {
         p.row1 = p.row0 + kAccPassRows;
         const int row_tiles = ((all_rows < p.row1 ? all_rows : p.row1) - p.row0 + 7) / 8;
-        constexpr int kRowBytes = D * (int)sizeof(T) * (sizeof(T) == 4 ? 2 : 1) + (sizeof(T) == 4 ? 12 : 8);
+        constexpr int kRowBytes = D * (int)sizeof(T) * (sizeof(T) == 4 ? 2 : 1) + 8;
         const size_t smem = (size_t)row_tiles * 8 * kRowBytes;
         if (!tc::set_smem_limit_once(reinterpret_cast<const void*>(accumulate_kernel<T, D>), kAccPassRows * kRowBytes)) return SPECPV_ERR_CUDA;
         SPECPV_LAUNCH((accumulate_kernel<T, D>), grid, 32 * kAccWarps, smem, stream, p);
