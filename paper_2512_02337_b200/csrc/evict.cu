@@ -59,6 +59,10 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
     pdl_begin(p.pdl);
     constexpr int kPieces = D * (int)sizeof(T) / 64;  // 16-byte pieces of a token per lane
     constexpr bool kF32 = sizeof(T) == 4;
+    // The matrix instruction truncates its sums: a score is smaller than it should be by some 5e-8 of itself at 64 channels of bfloat16,
+    // 1e-7 at 128, 6e-8 in float32 (measured; weights at scores of 10 came out 0.5e-6 to 1.3e-6 too small), and the log-sum-exp that it
+    // is compared with is made smaller by as much.
+    constexpr float kCut = kF32 ? 6e-8f : 8e-10f * D;
     extern __shared__ __align__(16) unsigned char acc_smem[];
     const int h = blockIdx.y, lb = blockIdx.z, b = lb % p.batch, l = lb / p.batch;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
@@ -71,16 +75,17 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
     constexpr int kTerms = kF32 ? 2 : 1;
     uint4* s_q = reinterpret_cast<uint4*>(acc_smem);  // [term][row tile][piece][lane]
     const int term_stride = row_tiles * kPieces * 32;
-    float* s_lse = reinterpret_cast<float*>(s_q + kTerms * term_stride);  // [row], in the unit of the products
-    int* s_end = reinterpret_cast<int*>(s_lse + row_tiles * 8);  // tokens that the row sees: none, if it adds nothing
+    float* s_lse = reinterpret_cast<float*>(s_q + kTerms * term_stride);  // [row], in the unit of the products; [row], what that lost
+    int* s_end = reinterpret_cast<int*>(s_lse + 2 * row_tiles * 8);  // tokens that the row sees: none, if it adds nothing
     __shared__ uint32_t s_idle;  // bit per row tile: such rows are among it
     __shared__ int s_odd;        // a query's element is infinite or NaN (float32)
     static_assert(kAccPassRows / 8 <= 32, "a bit per row tile");
+    const float scale = p.scale * 1.4426950408889634f;
     if (threadIdx.x == 0) s_idle = s_odd = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < row_tiles * 8; i += 32 * kAccWarps) {
         const int r = p.row0 + i, a = r / p.G;
-        float lse = 0.f;
+        float lse = 0.f, rest = 0.f;
         int row = -1, end = -1;
         if (i < rows) {
             row = p.accepted ? p.accepted[(size_t)b * p.A_max + a] : a;
@@ -91,12 +96,14 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
                 const float natural = p.lse[((size_t)lb * p.M_max + row) * p.Hq + h * p.G + r % p.G];
                 if (natural != -INFINITY) {
                     lse = natural / p.scale;
+                    if (isfinite(lse)) rest = (float)(((double)lse - (double)natural / (double)p.scale * (1.0 - (double)kCut)) * (double)scale);
                     end = seq_len - n + a + 1;
                 }
             }
         }
         if (end < 0) atomicOr(&s_idle, 1u << (i >> 3));
         s_lse[i] = lse;
+        s_lse[row_tiles * 8 + i] = rest;
         s_end[i] = end;
         const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.q) + (((size_t)lb * p.M_max + max(row, 0)) * p.Hq + h * p.G + r % p.G) * D);
 #pragma unroll
@@ -122,7 +129,6 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
     const size_t page_stride = (size_t)p.Hkv * p.bs * (D * sizeof(T) / 16);
     const int32_t* table = p.block_table + (size_t)b * p.max_blocks;
     float* acc = p.acc + (((size_t)(p.layer0 + l) * p.batch + b) * p.Hkv + h) * (size_t)p.max_blocks * p.bs;
-    const float scale = p.scale * 1.4426950408889634f;
     // tiles of 16 tokens divide a page (of 16, 32 or 64): page and place by shifts
     auto entry_of = [&](int tile) { return tile < tile1 ? table[tile >> p.tiles_log2] : -1; };
     auto fetch = [&](int tile, int page, uint4 (&x)[2][kPieces]) {  // keys of tokens g and g + 8; whether they are there
@@ -156,7 +162,9 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
         auto weigh = [&](int rt, const float (&c)[4]) {
             const float2 lse = *reinterpret_cast<const float2*>(s_lse + rt * 8 + 2 * t);
             // the difference first: where a weight counts it is small, and so then is what the factor's rounding takes from it
-            float w[4] = {tc::ex2((c[0] - lse.x) * scale), tc::ex2((c[1] - lse.y) * scale), tc::ex2((c[2] - lse.x) * scale), tc::ex2((c[3] - lse.y) * scale)};
+            const float2 rest = *reinterpret_cast<const float2*>(s_lse + (row_tiles + rt) * 8 + 2 * t);
+            float w[4] = {tc::ex2(fmaf(c[0] - lse.x, scale, rest.x)), tc::ex2(fmaf(c[1] - lse.y, scale, rest.y)),
+                          tc::ex2(fmaf(c[2] - lse.x, scale, rest.x)), tc::ex2(fmaf(c[3] - lse.y, scale, rest.y))};
             if (!all_seen || (idle >> rt & 1)) {  // (by choice, not by a weight of 0: the key may be infinite)
                 const int2 end = *reinterpret_cast<const int2*>(s_end + rt * 8 + 2 * t);
                 if (token >= end.x) w[0] = 0.f;
@@ -418,7 +426,7 @@ static specpv_status launch_accumulate_typed(AccumulateParams p, int n_layers, i
     for (p.row0 = 0; p.row0 < all_rows; p.row0 += kAccPassRows) {
         p.row1 = p.row0 + kAccPassRows;
         const int row_tiles = ((all_rows < p.row1 ? all_rows : p.row1) - p.row0 + 7) / 8;
-        constexpr int kRowBytes = D * (int)sizeof(T) * (sizeof(T) == 4 ? 2 : 1) + 8;
+        constexpr int kRowBytes = D * (int)sizeof(T) * (sizeof(T) == 4 ? 2 : 1) + 12;
         const size_t smem = (size_t)row_tiles * 8 * kRowBytes;
         if (!tc::set_smem_limit_once(reinterpret_cast<const void*>(accumulate_kernel<T, D>), kAccPassRows * kRowBytes)) return SPECPV_ERR_CUDA;
         SPECPV_LAUNCH((accumulate_kernel<T, D>), grid, 32 * kAccWarps, smem, stream, p);
