@@ -53,12 +53,6 @@ __device__ __forceinline__ int element_shift(int e) { return 4 * (e >> 1) + 16 *
 __device__ __forceinline__ uint32_t rotated(uint32_t w) { return __funnelshift_l(w, w, 3); }
 __device__ __forceinline__ uint32_t unrotated(uint32_t w) { return __funnelshift_r(w, w, 3); }
 
-// what one element stands for
-__device__ __forceinline__ float value_of(uint32_t w, int e, uint16_t scale, uint16_t offset) {
-    const uint32_t n = unrotated(w) >> element_shift(e) & 15u;
-    return lower(fma_bf16x2(0x4180u | n << 3, scale, offset));
-}
-
 // A row's scale and offset from its smallest and largest element, and the code of an element.  A row whose range or offset bfloat16
 // cannot hold is stored as NaN, and so is one whose `lo` or `hi` is infinite or NaN.
 struct Row {
