@@ -377,7 +377,8 @@ typedef struct {
 
 /* specpv_verify_full over a cache in 4 bits: the same arguments, masks, outputs and workspace; M_max = 1 is plain decoding.
  * A row that sees nothing (an empty cache and an empty row of the mask) gets out = 0 and lse = -infinity.  Infinities and NaN in
- * k_new and v_new reach the rows that see their token and no others. */
+ * k_new and v_new reach the rows that see their token and no others.  bfloat16: weights are rounded to bfloat16 once, for their product
+ * with the values; scores, sums and lse are float32.  float32: all of it is. */
 specpv_status specpv_verify_full_q4(const specpv_config *cfg, int layer0, int n_layers, const void *q, const void *k_new,
                                     const void *v_new, const uint64_t *tree_mask, const int32_t *q_lens, int M_max,
                                     const specpv_paged_q4 *full, void *out, float *lse, void *workspace,

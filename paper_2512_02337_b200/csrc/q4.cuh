@@ -51,7 +51,6 @@ __device__ __forceinline__ float upper(uint32_t pair) { return __uint_as_float(p
 // place of element e in a word before its rotation, and the rotation
 __device__ __forceinline__ int element_shift(int e) { return 4 * (e >> 1) + 16 * (e & 1); }
 __device__ __forceinline__ uint32_t rotated(uint32_t w) { return __funnelshift_l(w, w, 3); }
-__device__ __forceinline__ uint32_t unrotated(uint32_t w) { return __funnelshift_r(w, w, 3); }
 
 // A row's scale and offset from its smallest and largest element, and the code of an element.  A row whose range or offset bfloat16
 // cannot hold is stored as NaN, and so is one whose `lo` or `hi` is infinite or NaN.

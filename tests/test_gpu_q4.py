@@ -507,3 +507,43 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for c, w in zip(calls, want):
         assert torch.equal(c[4], w) and B.specpv_poll_status(c[5])[0] == 0
+
+
+def test_two_graphs_over_one_workspace():
+    """Captured calls of both kernels, replayed in turn on one stream, each against a cache that grows between replays."""
+    rng = np.random.default_rng(1)
+    cfg = config(1, 8, 2, 128, 64, "bf16")
+    q4 = Q.Q4(1, 2, 128, 64, [2000], max_blocks=40)
+    cache = q4.cache(B, max_seq_len=40 * 64)
+    ws = B.new_workspace(cfg, 1, 1, 40 * 64, 40)
+    stream = torch.cuda.Stream()
+    calls = []
+    for M in (1, 40):
+        q, _ = rows(rng, (1, 1, M, 8, 128), "bf16")
+        k, _ = rows(rng, (1, 1, M, 2, 128), "bf16")
+        _, mask = random_masks(rng, 1, M)
+        calls.append((M, q, k, mask, torch.zeros_like(q), torch.zeros(1, 1, M, 8, device="cuda")))
+
+    def run(c):
+        M, q, k, mask, out, lse = c
+        B.specpv_verify_full_q4(cfg, 0, 1, q, k, k, mask, None, M, cache, out, lse, ws)
+
+    graphs = []
+    with torch.cuda.stream(stream):
+        for c in calls:
+            run(c)
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1], stream=stream):
+                run(c)
+    one = torch.ones(1, dtype=torch.int32, device="cuda")
+    for step in range(6):
+        for c, graph in zip(calls, graphs):
+            with torch.cuda.stream(stream):
+                graph.replay()
+                replayed = c[4].clone(), c[5].clone()
+                run(c)
+            torch.cuda.synchronize()
+            assert torch.equal(replayed[0], c[4]) and torch.equal(replayed[1], c[5])
+            B.specpv_commit_accepted_q4(cfg, 0, 1, c[2], c[2], c[0], None, one, 1, cache, None, None, None, None, ws)
+            torch.cuda.synchronize()
+    assert cache.seq_lens.tolist() == [2012] and B.specpv_poll_status(ws)[0] == 0
