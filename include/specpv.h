@@ -355,8 +355,10 @@ specpv_status specpv_verify_full_offloaded(const specpv_config *cfg, int layer0,
 /* ---- Full KV cache in 4 bits -----------------------------------------------------------------------
  * (No counterpart in the paper.)  A full cache that takes d + 8 bytes per token and KV head instead of 4 d: 136 against 512
  * at 128 channels of bfloat16.  Every row (a token's key or value of one KV head) is quantised by itself:
- *   scale = bfloat16((max - min) / 15),  offset = bfloat16(min - 16 scale),  code n = the nearest of 0 .. 15 (ties to even)
- * and code n stands for bfloat16((16 + n) * scale + offset), rounded once.  A row that holds an infinity or a NaN, or whose range
+ *   scale = bfloat16((max - min) * r),  offset = bfloat16(min - 16 scale),  code n = the nearest of 0 .. 15 (ties to even) to
+ * (element - (offset + 16 scale)) / scale, where r is the float32 nearest to 1/15 (a product, not a quotient: the two round apart in one
+ * row of float32 in 85000) and every operation is rounded to float32;
+ * code n stands for bfloat16((16 + n) * scale + offset), rounded once.  A row that holds an infinity or a NaN, or whose range
  * bfloat16 cannot hold, is stored as NaN.  Attention, summaries and the partial cache taken out of it all see these bfloat16 values.
  *
  *   pool   [n_layers][n_pages][Hkv][bs (d + 8) bytes], a page of a KV head being

@@ -58,9 +58,9 @@ struct Row {
     float scale, base;  // in float32, for the codes; base = what code 0 stands for before its rounding
     uint16_t scale16, offset16;
 };
-// (x - base) / scale, and a range / 15, are IEEE quotients, in float32 to nearest.  So is RN(q + r i) with i a reciprocal of the divisor b
-// good to 2^-22 of itself, q = RN(a i) and r = a - q b: the dividend a has 24 significant bits and b at most 8 (it is a bfloat16, or 15), so that
-// r, 2^-21 of a at most and a multiple of the last places of q and b, has 12 bits and is exact; q + r i is then a / b but for 2^-43 of it, and
+// (x - base) / scale is the IEEE quotient, in float32 to nearest.  So is RN(q + r i) with i a reciprocal of the divisor b good to 2^-22 of
+// itself, q = RN(a i) and r = a - q b: the dividend a has 24 significant bits and b at most 8 (it is a bfloat16), so that r, 2^-21 of a at
+// most and a multiple of the last places of q and b, has 12 bits and is exact; q + r i is then a / b but for 2^-43 of it, and
 // nearer than 2^-33 of itself a / b comes to no number half-way between two of float32: such a number has 25 bits, its product with b a
 // last place 2^-33 of it or more, and is not a, which would have 25 bits as well.  Outside of kLeast .. kMost, where the reciprocal or the remainder
 // may underflow, they are divided.
@@ -77,7 +77,7 @@ __device__ __forceinline__ float quotient(float a, float b, float inv) {
 __device__ __forceinline__ Row row_of(float lo, float hi) {
     Row r;
     const float range = __fsub_rn(hi, lo);
-    const __nv_bfloat16 s = __float2bfloat16_rn(range > kLeast && range < kMost ? quotient(range, 15.f, 1.f / 15.f) : __fdiv_rn(range, 15.f));
+    const __nv_bfloat16 s = __float2bfloat16_rn(__fmul_rn(range, 1.f / 15.f));
     r.scale = __bfloat162float(s);
     const __nv_bfloat16 c = __float2bfloat16_rn(__fsub_rn(lo, 16.f * r.scale));  // (16 s is exact)
     const float offset = __bfloat162float(c);
