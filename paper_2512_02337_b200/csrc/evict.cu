@@ -367,13 +367,14 @@ __global__ void __launch_bounds__(kCloseThreads, 2) close_up_kernel(EvictParams 
     publish(1, t1, e1);
     __syncthreads();
     load(0, buf[0]);
+    __syncthreads();  // every thread has taken round 0's rows: round 2's come to their place
     auto round = [&](int i, uint4 (&now)[kCloseLoads], uint4 (&next)[kCloseLoads]) {
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // this round's rows have been read
         uint32_t dst[kCloseLoads];
 #pragma unroll
         for (int u = 0; u < kCloseLoads; ++u) dst[u] = to[u];
         load(i + 1, next);
-        publish(i + 2, token2, pages2);  // (the rows of round i have been taken from their place, by every thread: see the barrier below)
+        publish(i + 2, token2, pages2);  // (every thread has taken round i's rows from this place: the barrier below, of the round before, or the one above)
         pages2 = pages_of(i + 3, token3);
         token2 = token3;
         token3 = index_of(i + 4);
