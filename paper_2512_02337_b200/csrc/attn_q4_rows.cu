@@ -59,7 +59,7 @@ struct RowsParams {
     void* out;
     float* lse;
     float* part_o;   // [lb][Hkv][slots][R_max][d]
-    float* part_ml;  // [lb][Hkv][slots][R_max][2], natural logarithm
+    float* part_ml;  // [lb][Hkv][slots][R_max][2], the reference in units of log2, unrounded: the merge takes differences of them
     void* workspace;
     int layer0, batch, M_max, mask_words, Hq, Hkv, G, bs, bs_log2, max_blocks, n_pages;
     int n_layers, n_slots;
@@ -599,7 +599,7 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
             p.part_o[to * D + c] = o;
             if (c == 0) {
                 // nothing seen: -infinity; a NaN has to survive the merge, which leaves out what weighs nothing
-                p.part_ml[to * 2] = total == 0.f ? -INFINITY : total != total ? INFINITY : s_top[r] * kLn2;
+                p.part_ml[to * 2] = total == 0.f ? -INFINITY : total != total ? INFINITY : s_top[r];
                 p.part_ml[to * 2 + 1] = total;
             }
         }

@@ -52,6 +52,7 @@ struct SimtParams {
     void* workspace;
     int layer0, batch, M_max, mask_words, Hq, Hkv, G, bs, max_blocks, n_pages;
     int n_splits, row_tiles;
+    int ml_log2;  // part_ml holds maxima in units of log2 (launch_merge_splits); else natural ones
     int pdl;  // set by launch_pdl_if
     float scale;
 };
@@ -447,7 +448,7 @@ __global__ void __launch_bounds__(kMergeThreads) merge_splits_kernel(SimtParams 
     for (int o = kRowThreads / 2; o > 0; o >>= 1) m_all = fmaxf(m_all, __shfl_xor_sync(members, m_all, o));
     float w_mine = 0.f, l_mine = 0.f;
     if (mine.x != -INFINITY) {  // a split that saw no token weighs nothing
-        w_mine = expf(mine.x - m_all);
+        w_mine = p.ml_log2 ? tc::ex2(mine.x - m_all) : expf(mine.x - m_all);
         l_mine = mine.y * w_mine;
     }
     float l_all = 0.f;
@@ -485,7 +486,7 @@ __global__ void __launch_bounds__(kMergeThreads) merge_splits_kernel(SimtParams 
     dst[1] = from_float<TO>(o.y * inv);
     dst[2] = from_float<TO>(o.z * inv);
     dst[3] = from_float<TO>(o.w * inv);
-    if (p.lse && lane == 0) p.lse[row] = m_all + logf(l_all);
+    if (p.lse && lane == 0) p.lse[row] = p.ml_log2 ? fmaf(m_all, kLn2, logf(l_all)) : m_all + logf(l_all);
 }
 
 template <typename TO, int D>
@@ -537,7 +538,7 @@ static SimtParams simt_params(const AttnArgs& a) {
 
 specpv_status launch_merge_splits(const AttnArgs& a, int n_splits, float* part_o, float* part_ml, cudaStream_t stream) {
     SimtParams p = simt_params(a);
-    p.n_splits = n_splits; p.part_o = part_o; p.part_ml = part_ml;
+    p.n_splits = n_splits; p.part_o = part_o; p.part_ml = part_ml; p.ml_log2 = 1;
     if (a.g.d == 64) return a.g.out_f32 ? launch_merge<float, 64>(a, p, stream) : launch_merge<__nv_bfloat16, 64>(a, p, stream);
     return a.g.out_f32 ? launch_merge<float, 128>(a, p, stream) : launch_merge<__nv_bfloat16, 128>(a, p, stream);
 }

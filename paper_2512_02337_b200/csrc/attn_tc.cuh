@@ -7,8 +7,6 @@ namespace specpv {
 
 constexpr int kTileTokens = 128;         // KV tokens per tile (128 / page size pages)
 constexpr int kD = 128;
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr float kSafeRowSum = 1.1529215e18f;  // 2^60: a tile's row sum below this cannot overflow the float32 sums
 

@@ -32,6 +32,8 @@ constexpr size_t kStatusBytes = 256;
 // sequence, KV head, group of 256 rows) of a call; zero between launches).  All scratch starts behind it.
 constexpr size_t kHeaderBytes = 256 * 1024;
 constexpr int kMaxQTokens = 128;      // M_max supported by the attention kernels (two mask words)
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kMaxSplitCtas = 8 * 148;  // the workspace holds split-KV partial results of this many CTAs (+ one per head)
 
 // ---- programmatic dependent launch ---------------------------------------------------------------
@@ -164,7 +166,7 @@ specpv_status launch_attention_tc(const AttnArgs& a, cudaStream_t stream);  // b
 bool attention_tc_supported(const AttnArgs& a);
 specpv_status launch_attention_q4_rows(const AttnArgs& a, cudaStream_t stream);  // bf16, a cache in 4 bits, few rows
 bool attention_q4_rows_wanted(const AttnArgs& a);
-// log-sum-exp merge of partial results [lb][Hkv][splits][M_max * G] (rows of d floats; natural-log maximum and sum) into out and lse
+// log-sum-exp merge of partial results [lb][Hkv][splits][M_max * G] (rows of d floats; maximum in units of log2, and sum) into out and lse
 specpv_status launch_merge_splits(const AttnArgs& a, int n_splits, float* part_o, float* part_ml, cudaStream_t stream);
 
 }  // namespace specpv

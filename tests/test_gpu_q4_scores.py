@@ -1,0 +1,56 @@
+"""Attention over a cache in 4 bits where scores, rows or values leave the ordinary: huge scores, NaN, infinities of no weight."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2512_02337_b200 import binding as B
+from tests import q4_util as Q
+from tests.test_gpu_q4 import config, random_masks, rows, torch_dtype
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("M", [1, 4, 8, 20])
+def test_parts_of_a_long_cache_weigh_what_their_scores_say(M, d):
+    """Scores of 5600 whose differences across the cache are a few units: parts of the cache are weighed by their references' difference,
+    and rounding a reference of that size costs 2e-4 of a weight.  Everything is exact here: keys are whole numbers up to 15 (scale 1),
+    the softmax scale makes scores whole powers of two's logarithms, so weights are powers of two."""
+    rng = np.random.default_rng(M + d)
+    Hq, Hkv, bs, n = 8, 2, 64, 5000
+    cfg = config(1, Hq, Hkv, d, bs, "bf16", out_f32=1, softmax_scale=float(np.float32(np.log(2.0))))
+    assert np.float32(cfg.softmax_scale) * np.float32(1.4426950408889634) == 1
+    blocks = -(-n // bs)
+    cache = B.CacheQ4(B.new_q4_pool(cfg, blocks), torch.randperm(blocks)[None].int().cuda(), torch.zeros(1, dtype=torch.int32, device="cuda"),
+                      blocks * bs)
+    key = rng.integers(0, 16, (n, Hkv, d)).astype(np.float64)
+    key[..., 0], key[..., d - 1] = 15, 0               # the row's range: scale 1, offset -16
+    key[..., 1] = (rng.integers(3, 15, (blocks, Hkv))).repeat(bs, 0)[:n]  # what tells tokens apart goes by the page
+    value = rng.integers(0, 16, (blocks, Hkv, d)).repeat(bs, 0)[:n].astype(np.float64)
+    value[..., 0], value[..., d - 1] = 15, 0
+    ws = B.new_workspace(cfg, 1, 1, blocks * bs, M)
+    k, v = (torch.from_numpy(x)[None, None].bfloat16().cuda().contiguous() for x in (key, value))
+    kv, vv = torch.zeros_like(k), torch.zeros_like(v)
+    B.specpv_commit_accepted_q4(cfg, 0, 1, k, v, n, None, torch.tensor([n], dtype=torch.int32, device="cuda"), n, cache, None, None, kv, vv, ws)
+    assert torch.equal(k, kv) and torch.equal(v, vv)
+    q64 = np.zeros((1, 1, M, Hq, d))
+    q64[..., 0], q64[..., 1] = 544, rng.choice([1.0, 0.5, -1.0], (1, 1, M, Hq))
+    q = torch.from_numpy(q64).bfloat16().cuda()
+    _, mask = random_masks(rng, 1, M, 0.0)             # of the step's tokens nothing is seen
+    new = torch.zeros(1, 1, M, Hkv, d, dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.zeros(1, 1, M, Hq, d, device="cuda"), torch.zeros(1, 1, M, Hq, device="cuda")
+    B.specpv_verify_full_q4(cfg, 0, 1, q, new, new, mask, None, M, cache, out, lse, ws)
+    assert B.specpv_poll_status(ws)[0] == 0
+    out, lse = out.cpu().double().numpy()[0, 0], lse.cpu().double().numpy()[0, 0]
+    for j in range(M):
+        for h in range(Hq):
+            s = key[:, h // 4] @ q64[0, 0, j, h]
+            w = np.exp2(s - s.max())
+            want = w @ value[:, h // 4] / w.sum()
+            # weights are powers of two or (half units) off by 2^-8 in bfloat16, of either sign, over 64 tokens of a page and more; numerator
+            # and denominator are sums in float32 of 5000 numbers, 2^-23 of each 64 tokens
+            half = q64[0, 0, j, h, 1] == 0.5
+            assert np.all(np.abs(out[j, h] - want) <= (2.0 ** -16 + (Q.HALF_BF16 if half else 0)) * want), (j, h)
+            # a reference times ln 2 (half a step of each), the logarithm, their sum
+            top = s.max() * np.log(2.0)
+            assert abs(lse[j, h] - (top + np.log(w.sum()))) <= 2 * 2.0 ** -23 * top
