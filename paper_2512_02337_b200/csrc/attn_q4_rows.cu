@@ -33,6 +33,9 @@ constexpr int kChunk = 64;               // tokens
 // 241, on the tcgen05 kernel 457 / 483 / 485; 32 rows in one CTA 552, as two CTAs of 16 459, there 486; 4096 tokens x 1 layer 43 / 26, there 16.)
 constexpr int kMaxRows = 16;
 constexpr float kRaise = 16.f;           // log2 of the weight from which references are raised
+// References from here on are coarser than 1.  Scores are then rounded to float32 before the reference, one of them, is taken off: the
+// difference of an unrounded product to its own rounding could pass kRaise, at 2^28 and more, and no reference would ever do.
+constexpr float kCoarse = 16777216.f;    // 2^24
 
 // rows of a CTA: 8 NT
 template <int D, int NT>
@@ -279,10 +282,18 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
             for (int c = 0; c < D / 16; ++c) acc[c][n][0] = acc[c][n][1] = acc[c][n][2] = acc[c][n][3] = 0.f;
         }
         const float scale = p.scale_log2;
+        auto any_coarse = [&](const float (&reference)[NT][2]) {
+            float largest = 0.f;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) largest = fmaxf(largest, fmaxf(fabsf(reference[n][0]), fabsf(reference[n][1])));
+            return __any_sync(0xffffffffu, largest >= kCoarse) != 0;
+        };
         const uint32_t mask = p.q4_mask, ones = p.q4_ones;
-        // (Two copies of the code: where a branch chose between opened codes and the step's own rows, every fragment was moved once more.)
-        auto work = [&](auto is_step, int i) {
-            constexpr bool step = decltype(is_step)::value;
+        // (Copies of the code: where a branch chose between opened codes and the step's own rows, every fragment was moved once more.  A branch
+        // that told coarse references apart cost 6 % over long caches, a copy 1 %: 445 -> 474, 450 us for four sequences of 96K to 128K x 4 layers.)
+        enum Outcome { kGaveUp, kDone, kTooCoarse };  // kTooCoarse: a reference has to be coarse, and nothing has been done
+        auto work = [&](auto is_step, auto is_coarse, int i) {
+            constexpr bool step = decltype(is_step)::value, coarse = decltype(is_coarse)::value;
             const int chunk = warp + i * kWarps;
             const uint32_t slot = (fills0 + i) % kStages, stage = ring + slot * S::kStageBytes;
             const int left = step ? M : seq_len - (begin + chunk) * kChunk;  // valid tokens of the chunk, if fewer than 64
@@ -297,7 +308,7 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
                     }
             }
             if constexpr (!step) {
-                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&full[warp][slot]), (fills0 + i) / kStages & 1, &abort_flag, p.workspace, 41))) return false;
+                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&full[warp][slot]), (fills0 + i) / kStages & 1, &abort_flag, p.workspace, 41))) return kGaveUp;
                 bad = bad_pages[warp][slot];
                 if (bad || left < kChunk) {
                     // Tokens behind a bad page id have no scales and offsets, nor (values) have those past the end: zeros.
@@ -406,14 +417,24 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
                             }
                         }
                     }
-                    float top = -INFINITY;
+                    float top = -INFINITY, rounded[NT][2];  // the rows' largest rounded scores
+                    if constexpr (coarse) {
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) rounded[n][0] = rounded[n][1] = -INFINITY;
+                    }
 #pragma unroll
                     for (int s = 0; s < kTogether; ++s)
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                cs[s][n][e] = fmaf(cs[s][n][e], scale, -m[n][e & 1]);
+                                if constexpr (coarse) {
+                                    cs[s][n][e] = __fmul_rn(cs[s][n][e], scale);
+                                    rounded[n][e & 1] = fmaxf(rounded[n][e & 1], cs[s][n][e]);
+                                    cs[s][n][e] = __fsub_rn(cs[s][n][e], m[n][e & 1]);
+                                } else {
+                                    cs[s][n][e] = fmaf(cs[s][n][e], scale, -m[n][e & 1]);
+                                }
                                 top = fmaxf(top, cs[s][n][e]);
                             }
                     if (look) {
@@ -437,21 +458,32 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
                                         cs[s][n][e + 2] -= m[n][e];
                                     }
                                 }
+                            if (!coarse && any_coarse(m)) return kTooCoarse;
                             look = false;
                         }
                     } else if (__any_sync(0xffffffffu, top > kRaise)) {
                         // references rise to the largest of these tokens; sums and accumulators follow, and the chunk starts over
+                        float risen[NT][2];
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                float rise = 0.f;
+                                float rise = coarse ? rounded[n][e] : 0.f;
+                                if constexpr (!coarse) {
 #pragma unroll
-                                for (int s = 0; s < kTogether; ++s) rise = fmaxf(rise, fmaxf(cs[s][n][e], cs[s][n][e + 2]));
+                                    for (int s = 0; s < kTogether; ++s) rise = fmaxf(rise, fmaxf(cs[s][n][e], cs[s][n][e + 2]));
+                                }
 #pragma unroll
                                 for (int o = 4; o < 32; o <<= 1) rise = fmaxf(rise, __shfl_xor_sync(0xffffffffu, rise, o));
-                                const float factor = ex2(-rise);
-                                m[n][e] += rise;
+                                risen[n][e] = coarse ? fmaxf(m[n][e], rise) : m[n][e] + rise;
+                            }
+                        if (!coarse && any_coarse(risen)) return kTooCoarse;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const float factor = ex2(m[n][e] - risen[n][e]);
+                                m[n][e] = risen[n][e];
                                 sum[n][e] *= factor;
 #pragma unroll
                                 for (int d = 0; d < D / 16; ++d) {
@@ -481,6 +513,7 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) m[n][e] = reference(most[n][e]);
+                    if (!coarse && any_coarse(m)) return kTooCoarse;
                     look = false;
                     again = true;
                 }
@@ -530,14 +563,24 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
                 copy(i + kStages, next_entry);
                 next_entry = entry_of(i + kStages + 1);
             }
-            return true;
+            return kDone;
         };
         int i = 0;
-        bool ok = true;
+        Outcome outcome = kDone;
+        auto walk = [&](auto is_coarse) {
 #pragma unroll 1
-        for (; ok && warp + i * kWarps < n_ctx; ++i) ok = work(std::false_type(), i);
+            for (; warp + i * kWarps < n_ctx; ++i)
+                if ((outcome = work(std::false_type(), is_coarse, i)) != kDone) return;
+            if (warp + i * kWarps < n_chunks) outcome = work(std::true_type(), is_coarse, i);
+        };
+        walk(std::false_type());
+        if (outcome == kTooCoarse) {  // from this chunk on; a first one is looked at anew
+            if (i == 0)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) m[n][0] = m[n][1] = 0.f;
+            walk(std::true_type());
+        }
         fills = fills0 + i;
-        if (ok && warp + i * kWarps < n_chunks) work(std::true_type(), i);
 
         // ---- the warps meet ----
 #pragma unroll

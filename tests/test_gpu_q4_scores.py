@@ -54,3 +54,44 @@ def test_parts_of_a_long_cache_weigh_what_their_scores_say(M, d):
             # a reference times ln 2 (half a step of each), the logarithm, their sum
             top = s.max() * np.log(2.0)
             assert abs(lse[j, h] - (top + np.log(w.sum()))) <= 2 * 2.0 ** -23 * top
+
+
+@pytest.mark.parametrize("dtype,M", [("bf16", 1), ("bf16", 2), ("bf16", 4), ("fp32", 3)])
+@pytest.mark.parametrize("log2_q", [28, 29, 33, 60, 100])
+def test_scores_far_past_the_whole_numbers_of_float32(dtype, M, log2_q):
+    """Scores of 2^26 to 2^100, whose neighbours in float32 lie 8 to 2^77 apart: references climb from tile to tile and come to rest.  A query
+    is a power of two in one channel, and the key value of that channel decides: a row is the mean of the values of its largest keys,
+    wherever they are."""
+    rng = np.random.default_rng(log2_q + M)
+    Hq, Hkv, d, bs, n, batch = 32, 8, 64, 64, 3000, 24  # every sequence over the same pages; warps go from chunk to chunk
+    cfg = config(1, Hq, Hkv, d, bs, dtype, out_f32=1)
+    q4 = Q.Q4(1, Hkv, d, bs, [n], seed=3)
+    cache = q4.cache(B)
+    cache.block_table = cache.block_table.expand(batch, -1).contiguous()
+    cache.seq_lens = cache.seq_lens.expand(batch).contiguous()
+    q64 = np.zeros((1, batch, M, Hq, d))
+    channel = rng.integers(0, d, (batch, M, Hq))
+    np.put_along_axis(q64[0], channel[..., None], 2.0 ** log2_q * rng.choice([-1.0, 1.0], (batch, M, Hq, 1)), -1)
+    q = torch.from_numpy(q64).to(torch_dtype(dtype)).cuda()
+    k, k64 = rows(rng, (1, batch, M, Hkv, d), "bf16")
+    v, v64 = rows(rng, (1, batch, M, Hkv, d), "bf16")
+    k, v = k.to(q.dtype), v.to(q.dtype)
+    seen, mask = random_masks(rng, batch, M)
+    out, lse = torch.zeros(1, batch, M, Hq, d, device="cuda"), torch.zeros(1, batch, M, Hq, device="cuda")
+    ws = B.new_workspace(cfg, 1, batch, n, M)
+    B.specpv_verify_full_q4(cfg, 0, 1, q, k, v, mask, None, M, cache, out, lse, ws)
+    assert B.specpv_poll_status(ws)[0] == 0
+    out, lse = out.cpu().double().numpy()[0], lse.cpu().double().numpy()[0]
+    for b in range(batch):
+        for h in range(Hq):
+            kk, vv = (np.concatenate([x[0][0, h // 4], y[0, b, :, h // 4]]) for x, y in ((q4.k, k64), (q4.v, v64)))
+            for j in range(M):
+                there = np.concatenate([np.ones(n, bool), seen[b, j]])
+                s = kk[:, channel[b, j, h]] * q64[0, b, j, h, channel[b, j, h]] / 8
+                top = s[there].max()
+                w = np.where(there & (s == top), 1.0, 0.0)  # (the next key, 2^-8 of it or more below, weighs exp(-2^18) or less)
+                want = w @ vv / w.sum()
+                # equal scores, rounded alike: weights of 1, sums of a few values in float32
+                assert np.all(np.abs(out[b, j, h] - want) <= 2.0 ** -20 * (w @ np.abs(vv) / w.sum()))
+                # the score: scaled by a float32 factor and back, three roundings, which also hold the logarithm
+                assert abs(lse[b, j, h] - (top + np.log(w.sum()))) <= 2.0 ** -21 * np.abs(top)
