@@ -64,6 +64,9 @@ struct Shape {
 };
 constexpr int kMaxStages = 10;
 constexpr int kShortWalk = 4;  // tiles per CTA
+// kQ4: references from here on are coarser than 1.  Scores are then rounded to float32 before the reference, one of them, is taken off: the
+// difference of an unrounded product to its own rounding passes the exponential's range at 2^31.
+constexpr float kCoarse = 16777216.f;  // 2^24
 
 using namespace tc;
 
@@ -613,6 +616,7 @@ __device__ __forceinline__ void softmax(const TcParams& p, const Job& c, Barrier
         if (p.mask_words > 1) mask_hi = mrow[1];
     }
     float m_run = -INFINITY, l_run = 0.f;
+    bool coarse = false;  // kQ4: a row of the warp has a reference of kCoarse or more
     bool ok = true;
     const float2 sc2 = make_float2(p.scale_log2, p.scale_log2), sc2_lo = make_float2(p.scale_log2_lo, p.scale_log2_lo);
     // One row tile (the form of short calls): the first pass of the loop is a dry run over zeros by stream 1, whose S comes
@@ -708,7 +712,7 @@ __device__ __forceinline__ void softmax(const TcParams& p, const Job& c, Barrier
         // from tensor memory on the general path, which brings m_run up to date.  A short walk of the two-term form, whose fast path
         // would be met with cold code, stays on the general path (40 rows x 4 of 64 channels, 4 tiles per CTA: 17.8 -> 17.3 us).
         float l_add = 0.f;
-        bool general = (kOne ? j <= first_tile : j == first_tile) || masked || (kOne && kSplit && n_tiles <= kShortWalk);
+        bool general = (kOne ? j <= first_tile : j == first_tile) || masked || (kOne && kSplit && n_tiles <= kShortWalk) || (kQ4 && coarse);
         if (!general) {
             l_add = exp_row(m_run);
             const bool bad = !(l_add < kSafeRowSum) || m_run == -INFINITY;
@@ -765,7 +769,18 @@ __device__ __forceinline__ void softmax(const TcParams& p, const Job& c, Barrier
                     m_run = m_tile;
                 }
             }
-            l_add = exp_row(m_run == -INFINITY ? 0.f : m_run);
+            float m_use = m_run == -INFINITY ? 0.f : m_run;
+            if constexpr (kQ4) {
+                coarse = __any_sync(0xffffffffu, fabsf(m_use) >= kCoarse);
+                if (coarse) {  // exp_row's product is then off by 2^-24 of a difference, not of a score
+                    const float back = 1.f / p.scale_log2;  // (finite: a scale below 2^-104 makes no score of 2^24)
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        v[i] = __float_as_uint(__fmul_rn(__fsub_rn(__fmul_rn(__uint_as_float(v[i]), p.scale_log2), m_use), back));
+                    m_use = 0.f;
+                }
+            }
+            l_add = exp_row(m_use);
         }
         if (dry) {
             l_run = l_add < 0.f ? l_add : 0.f;  // never negative: zero again, and the dry run's sums are not dead code

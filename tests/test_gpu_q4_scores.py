@@ -56,14 +56,15 @@ def test_parts_of_a_long_cache_weigh_what_their_scores_say(M, d):
             assert abs(lse[j, h] - (top + np.log(w.sum()))) <= 2 * 2.0 ** -23 * top
 
 
-@pytest.mark.parametrize("dtype,M", [("bf16", 1), ("bf16", 2), ("bf16", 4), ("fp32", 3)])
+@pytest.mark.parametrize("dtype,M", [("bf16", 1), ("bf16", 2), ("bf16", 4), ("bf16", 20), ("bf16", 40), ("fp32", 3)])
 @pytest.mark.parametrize("log2_q", [28, 29, 33, 60, 100])
 def test_scores_far_past_the_whole_numbers_of_float32(dtype, M, log2_q):
     """Scores of 2^26 to 2^100, whose neighbours in float32 lie 8 to 2^77 apart: references climb from tile to tile and come to rest.  A query
     is a power of two in one channel, and the key value of that channel decides: a row is the mean of the values of its largest keys,
     wherever they are."""
     rng = np.random.default_rng(log2_q + M)
-    Hq, Hkv, d, bs, n, batch = 32, 8, 64, 64, 3000, 24  # every sequence over the same pages; warps go from chunk to chunk
+    # every sequence over the same pages; warps go from chunk to chunk, CTAs from tile to tile
+    Hq, Hkv, d, bs, n, batch = 32, 8, 64, 64, 3000, 24 if M < 8 else 4
     cfg = config(1, Hq, Hkv, d, bs, dtype, out_f32=1)
     q4 = Q.Q4(1, Hkv, d, bs, [n], seed=3)
     cache = q4.cache(B)
