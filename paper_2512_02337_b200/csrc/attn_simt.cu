@@ -395,7 +395,8 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(SimtParams p) {
                 *reinterpret_cast<float4*>(p.part_o + prow * D + c / 4 * 64 + 4 * tx) =
                     make_float4(acc[i][c], acc[i][c + 1], acc[i][c + 2], acc[i][c + 3]);
             if (tx == 0) {
-                p.part_ml[prow * 2] = m_run[i];
+                // (kQ4: a NaN has to survive the merge, which leaves out what has seen nothing)
+                p.part_ml[prow * 2] = kQ4 && l_run[i] != l_run[i] ? INFINITY : m_run[i];
                 p.part_ml[prow * 2 + 1] = l_run[i];
             }
         }

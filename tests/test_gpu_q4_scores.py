@@ -96,3 +96,48 @@ def test_scores_far_past_the_whole_numbers_of_float32(dtype, M, log2_q):
                 assert np.all(np.abs(out[b, j, h] - want) <= 2.0 ** -20 * (w @ np.abs(vv) / w.sum()))
                 # the score: scaled by a float32 factor and back, three roundings, which also hold the logarithm
                 assert abs(lse[b, j, h] - (top + np.log(w.sum()))) <= 2.0 ** -21 * np.abs(top)
+
+
+def verify(dtype, Hq, Hkv, d, q4, q, k, v, mask, M, out_f32=0):
+    cfg = config(1, Hq, Hkv, d, q4.bs, dtype, out_f32=out_f32)
+    out = torch.full((1, 1, M, Hq, d), 7.0, dtype=torch.float32 if out_f32 else torch_dtype(dtype), device="cuda")
+    lse = torch.full((1, 1, M, Hq), 7.0, device="cuda")
+    ws = B.new_workspace(cfg, 1, 1, max(q4.lens), M)
+    B.specpv_verify_full_q4(cfg, 0, 1, q, k, v, mask, None, M, q4.cache(B), out, lse, ws)
+    assert B.specpv_poll_status(ws)[0] == 0
+    return out[0, 0].cpu(), lse[0, 0].cpu()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("M", [1, 3, 20])
+@pytest.mark.parametrize("where", ["q", "k", "cache"])
+def test_nan_among_the_parts_of_a_long_cache(dtype, d, M, where):
+    """A cache long enough to be split many times: a NaN that is all that one of the parts sees is not left out when they meet."""
+    rng = np.random.default_rng(d + M)
+    Hq, Hkv, n = 8, 2, 2000
+    q4 = Q.Q4(1, Hkv, d, 64, [n], seed=2)
+    q, _ = rows(rng, (1, 1, M, Hq, d), dtype)
+    k, _ = rows(rng, (1, 1, M, Hkv, d), dtype)
+    v, _ = rows(rng, (1, 1, M, Hkv, d), dtype)
+    seen, mask = random_masks(rng, 1, M, 0.0)
+    seen[0, range(M), range(M)] = True  # every row sees itself alone
+    mask = torch.zeros_like(mask)
+    for j in range(M):
+        mask[0, j, j // 64] = 1 << (j % 64)
+    clean, clean_lse = verify(dtype, Hq, Hkv, d, q4, q, k, v, mask, M)
+    assert clean.isfinite().all() and clean_lse.isfinite().all()
+    hit = torch.zeros(M, Hq, dtype=torch.bool)
+    if where == "q":
+        q[0, 0, M - 1, 3, 5] = float("nan")
+        hit[M - 1, 3] = True
+    elif where == "k":
+        k[0, 0, M - 1, 1, 5] = float("nan")
+        hit[M - 1, 4:] = True
+    else:  # a cached key that was stored as NaN: all rows of its KV head see it
+        par = q4.pool[0, q4.table[0, 7], 0, 64 * d:].view(np.uint16).reshape(4, 64)
+        par[:2, 9] = 0x7FC0
+        hit[:, :4] = True
+    out, lse = verify(dtype, Hq, Hkv, d, q4, q, k, v, mask, M)
+    assert out[hit].isnan().all() and lse[hit].isnan().all()
+    assert torch.equal(out[~hit], clean[~hit]) and torch.equal(lse[~hit], clean_lse[~hit])
