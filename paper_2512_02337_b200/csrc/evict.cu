@@ -16,11 +16,14 @@ namespace {
 // tokens t that row i sees.  The keys are read once, at the rate of the memory (that is the bound), straight into the registers that
 // the warp-wide matrix instruction takes them from: a warp owns 16 tokens at a time, S^T [16 tokens x 8 rows] = K Q^T.  The sum over
 // channels may be taken in any order, so lane (g, t) keeps the 16 bytes at 16 (4 j + t) of tokens g and g + 8 as they come.  The
-// rows' queries wait in shared memory in the same order, 16 bytes a lane.  (98309 tokens x 8 heads x 12 layers, 28 rows: 416 us, 92 % of
-// the copy rate; 510 with one chain of products per row tile, keys moved from buffer to buffer and divisions by the page size.)
+// rows' queries wait in shared memory in the same order, 16 bytes a lane.  The instruction truncates its sums, so that it sums over 32
+// channels only and the rest is added in float32: the weights of 5000 tokens, 16 rows x 4 are off by 5.4e-7 and 6.8e-7 of themselves (64 and 128
+// channels; 5.9e-7 and 9.9e-7 with two chains over half the channels each).
+// (98309 tokens x 8 heads x 12 layers, 28 rows: 522 us a pass, 0.73 of the copy rate; 505 with the longer chains, a third more than 522 with 16
+// channels to a sum.)
 // float32: both factors as two terms of 11 bits, three products (m16n8k8), which leaves 2^-21 of a product, summed by the instruction
-// (which truncates) over 16 channels only and then in float32 (1.5e-6 of a weight was lost with one chain of 128 channels); bound by forming the
-// terms and by the products (4261 tokens x 8 heads x 8 layers, 20 rows 74 us, 21 for its bytes; with terms formed per row tile and every
+// over 16 channels only (1.5e-6 of a weight was lost with one chain of 128 channels, 0.9e-6 now); bound by forming the
+// terms and by the products (4261 tokens x 8 heads x 8 layers, 20 rows 77 us, 21 for its bytes; with terms formed per row tile and every
 // element tested for infinity 145).  A token's sum over the rows is formed in a fixed order: the same at every run.
 // ---------------------------------------------------------------------------------------------
 constexpr int kAccWarps = 8;
@@ -59,10 +62,6 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
     pdl_begin(p.pdl);
     constexpr int kPieces = D * (int)sizeof(T) / 64;  // 16-byte pieces of a token per lane
     constexpr bool kF32 = sizeof(T) == 4;
-    // The matrix instruction truncates its sums: a score is smaller than it should be by some 5e-8 of itself at 64 channels of bfloat16,
-    // 1e-7 at 128, 6e-8 in float32 (measured; weights at scores of 10 came out 0.5e-6 to 1.3e-6 too small), and the log-sum-exp that it
-    // is compared with is made smaller by as much.
-    constexpr float kCut = kF32 ? 6e-8f : 8e-10f * D;
     extern __shared__ __align__(16) unsigned char acc_smem[];
     const int h = blockIdx.y, lb = blockIdx.z, b = lb % p.batch, l = lb / p.batch;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
@@ -96,7 +95,7 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
                 const float natural = p.lse[((size_t)lb * p.M_max + row) * p.Hq + h * p.G + r % p.G];
                 if (natural != -INFINITY) {
                     lse = natural / p.scale;
-                    if (isfinite(lse)) rest = (float)(((double)lse - (double)natural / (double)p.scale * (1.0 - (double)kCut)) * (double)scale);
+                    if (isfinite(lse)) rest = (float)(((double)lse - (double)natural / (double)p.scale) * (double)scale);
                     end = seq_len - n + a + 1;
                 }
             }
@@ -178,15 +177,16 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
         if constexpr (!kF32) {
 #pragma unroll 1
             for (int rt = 0; rt < row_tiles; ++rt) {
-                float c[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};  // two chains of products
+                float c[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int j = 0; j < kPieces; ++j) {
                     const uint4 q = s_q[(rt * kPieces + j) * 32 + lane];
-                    mma_bf16(c, now[0][j].x, now[1][j].x, now[0][j].y, now[1][j].y, q.x, q.y);
-                    mma_bf16(c1, now[0][j].z, now[1][j].z, now[0][j].w, now[1][j].w, q.z, q.w);
-                }
+                    float part[4] = {0.f, 0.f, 0.f, 0.f};  // of 32 channels
+                    mma_bf16(part, now[0][j].x, now[1][j].x, now[0][j].y, now[1][j].y, q.x, q.y);
+                    mma_bf16(part, now[0][j].z, now[1][j].z, now[0][j].w, now[1][j].w, q.z, q.w);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) c[e] += c1[e];
+                    for (int e = 0; e < 4; ++e) c[e] += part[e];
+                }
                 weigh(rt, c);
             }
         } else {
