@@ -81,7 +81,7 @@ __device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
 // 264 us, against 384 with four channels at a time fetched and opened like the rows of an ordinary cache; 136 with warps that have no
 // row left idle and splits in whole waves.)  Also, a row that sees nothing comes out as zeros, and
 // an infinity or NaN among the step's own values reaches the rows that see its token and no others: such an element takes no part
-// in the products (0 times it would be NaN) and is added to the sums of the rows that see it, whose weight of it is positive.
+// in the products (0 times it would be NaN) and is added at the end to the sums of the rows that see it, whose weight of it is positive.
 template <typename T, typename TO, int D, bool kQ4>
 __global__ void __launch_bounds__(kThreads) attn_simt_kernel(SimtParams p) {
     pdl_begin(p.pdl);
@@ -147,6 +147,8 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(SimtParams p) {
     uint32_t key_words[kKeyWords], key_par = 0, value_par = 0;
     uint2 value_words[kGroups];
     __shared__ __align__(8) uint32_t s_value_par[kTok];  // scale | offset << 16
+    __shared__ int s_odd;  // one of the step's values is infinite or NaN
+    if (kQ4 && tid == 0) s_odd = 0;
     auto fetch = [&](int tile) {
         const T *ks = nullptr, *vs = nullptr;
         if (kQ4 && tile < ctx_tiles) {
@@ -220,7 +222,6 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(SimtParams p) {
     for (int tile = tile_begin; tile < tile_end; ++tile) {
         const bool is_new = tile >= ctx_tiles;
         const int tok0 = (is_new ? tile - ctx_tiles : tile) * kTok;
-        int odd = 0;  // kQ4: the tile holds an infinite or NaN value
         __syncthreads();  // the previous tile has been read
         if (kQ4 && !is_new) {
 #pragma unroll
@@ -257,7 +258,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(SimtParams p) {
                     float v[4] = {vbuf[i].x, vbuf[i].y, vbuf[i].z, vbuf[i].w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        odd |= !isfinite(v[e]);
+                        if (!isfinite(v[e])) s_odd = 1;
                         v[e] = isfinite(v[e]) ? v[e] : 0.f;
                     }
                     vbuf[i] = make_float4(v[0], v[1], v[2], v[3]);
@@ -266,8 +267,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(SimtParams p) {
             }
         }
         if (sc == 0) s_exists[st] = exists;
-        if (kQ4 && is_new) odd = __syncthreads_or(odd);
-        else __syncthreads();
+        __syncthreads();
         if (tile + 1 < tile_end) fetch(tile + 1);
         if (row0 + tid / 32 * 8 >= R) continue;  // none of the warp's eight rows is there
         // S = Q K^T: rows 4 ty .. + 3, tokens 4 tx .. + 3.  Channels are summed in runs of 16, the runs then added: the
@@ -361,19 +361,19 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(SimtParams p) {
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int c = 0; c < CPT; ++c) acc[i][c] = fmaf(acc[i][c], corr[i], c % 2 ? tile_acc[i][c / 2].y : tile_acc[i][c / 2].x);
-        if (kQ4 && odd) {
-            for (int t = 0; t < kTok && tok0 + t < M; ++t)
+    }
+    if (kQ4 && tile_end > ctx_tiles && s_odd) {  // (set before the last tile's barrier)
+        for (int t = (max(tile_begin, ctx_tiles) - ctx_tiles) * kTok; t < min((tile_end - ctx_tiles) * kTok, M); ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (!(s_mask[4 * ty + i][(tok0 + t) >> 6] >> ((tok0 + t) & 63) & 1)) continue;
-                    const T* v = v_new + ((size_t)(tok0 + t) * p.Hkv + h) * D;
+            for (int i = 0; i < 4; ++i) {
+                if (!(s_mask[4 * ty + i][t >> 6] >> (t & 63) & 1)) continue;
+                const T* v = v_new + ((size_t)t * p.Hkv + h) * D;
 #pragma unroll
-                    for (int c = 0; c < CPT; ++c) {
-                        const float x = to_float<T>(v[c / 4 * 64 + 4 * tx + c % 4]);
-                        if (!isfinite(x)) acc[i][c] += x;
-                    }
+                for (int c = 0; c < CPT; ++c) {
+                    const float x = to_float<T>(v[c / 4 * 64 + 4 * tx + c % 4]);
+                    if (!isfinite(x)) acc[i][c] += x;
                 }
-        }
+            }
     }
     // acc[i][c .. c + 3] are channels 16 c + 4 tx .. + 3 of row 4 ty + i
 #pragma unroll
@@ -450,6 +450,7 @@ __global__ void __launch_bounds__(kMergeThreads) merge_splits_kernel(SimtParams 
     float w_mine = 0.f, l_mine = 0.f;
     if (mine.x != -INFINITY) {  // a split that saw no token weighs nothing
         w_mine = p.ml_log2 ? tc::ex2(mine.x - m_all) : expf(mine.x - m_all);
+        if (p.q4_pool && w_mine < kLeastWeight) w_mine = kLeastWeight;
         l_mine = mine.y * w_mine;
     }
     float l_all = 0.f;

@@ -1119,6 +1119,7 @@ __global__ void __launch_bounds__(kMergeThreads) merge_tc_kernel(const __grid_co
             const float2 v = ml[(size_t)(c0 + lane) * p.R_pad];
             if (v.x != -INFINITY) {  // an empty split's partial O was never written: weight 0, not used
                 w_mine = ex2(v.x - m_all);
+                if (p.q4_pool && w_mine < kLeastWeight) w_mine = kLeastWeight;
                 l_mine = v.y * w_mine;
             }
         }

@@ -139,6 +139,10 @@ template <typename T> __device__ __forceinline__ T from_float(float v);
 template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+// Merging the parts of a cache in 4 bits: a part that has seen a token weighs this at least, the smallest float32.  Times a weight that
+// float32 takes for 0 its infinities would be lost; of its finite sums, 2^-149 is nothing.
+constexpr float kLeastWeight = 1.4012985e-45f;
+
 // ---- launchers implemented in the kernel files --------------------------------------------------
 struct AttnArgs {
     Geometry g;

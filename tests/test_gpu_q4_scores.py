@@ -92,8 +92,9 @@ def test_scores_far_past_the_whole_numbers_of_float32(dtype, M, log2_q):
                 top = s[there].max()
                 w = np.where(there & (s == top), 1.0, 0.0)  # (the next key, 2^-8 of it or more below, weighs exp(-2^18) or less)
                 want = w @ vv / w.sum()
-                # equal scores, rounded alike: weights of 1, sums of a few values in float32
-                assert np.all(np.abs(out[b, j, h] - want) <= 2.0 ** -20 * (w @ np.abs(vv) / w.sum()))
+                # equal scores, rounded alike: weights of 1, sums of a few values in float32.  Each of the other parts of the cache, 64 at most,
+                # weighs 2^-149 (so that infinite values come through) of sums of at most 3000 values of weight 2^16: 2^-149 2^6 2^12 2^16
+                assert np.all(np.abs(out[b, j, h] - want) <= 2.0 ** -20 * (w @ np.abs(vv) / w.sum()) + 2.0 ** -115 * np.abs(vv).max())
                 # the score: scaled by a float32 factor and back, three roundings, which also hold the logarithm
                 assert abs(lse[b, j, h] - (top + np.log(w.sum()))) <= 2.0 ** -21 * np.abs(top)
 
@@ -141,3 +142,34 @@ def test_nan_among_the_parts_of_a_long_cache(dtype, d, M, where):
     out, lse = verify(dtype, Hq, Hkv, d, q4, q, k, v, mask, M)
     assert out[hit].isnan().all() and lse[hit].isnan().all()
     assert torch.equal(out[~hit], clean[~hit]) and torch.equal(lse[~hit], clean_lse[~hit])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("M,n", [(1, 2000), (3, 2000), (20, 2000), (100, 200), (100, 2000)])
+def test_infinite_values_of_hardly_any_weight(dtype, d, M, n):
+    """An infinite value reaches the rows that see its token however little the token weighs: exp(-150) is no float32, but it is not 0."""
+    rng = np.random.default_rng(d + M)
+    Hq, Hkv = 8, 2
+    q4 = Q.Q4(1, Hkv, d, 64, [n], seed=2)
+    q, _ = rows(rng, (1, 1, M, Hq, d), dtype, 150.0)
+    k = torch.zeros(1, 1, M, Hkv, d, dtype=q.dtype, device="cuda")
+    k[..., M // 2:, :, :] = -q[0, 0, M // 2:, ::Hq // Hkv] / 150  # half of the step's tokens lie far below the others for their own rows
+    v, _ = rows(rng, (1, 1, M, Hkv, d), dtype)
+    seen = rng.random((M, M)) < 0.4
+    seen[range(M), range(M)] = True
+    words = np.zeros((1, M, (M + 63) // 64), np.uint64)
+    for j in range(M):
+        words[0, :, j // 64] |= seen[:, j].astype(np.uint64) << np.uint64(j % 64)
+    mask = torch.from_numpy(words.view(np.int64)).cuda()
+    clean, clean_lse = verify(dtype, Hq, Hkv, d, q4, q, k, v, mask, M)
+    token, channel = (M - 1, 0), (3, d - 1)
+    v[0, 0, M - 1, 0, 3], v[0, 0, 0, 1, d - 1] = float("inf"), -float("inf")
+    out, lse = verify(dtype, Hq, Hkv, d, q4, q, k, v, mask, M)
+    assert torch.equal(lse, clean_lse)
+    for h in range(Hq):
+        e = h // 4
+        hit = torch.from_numpy(seen[:, token[e]])
+        assert torch.all(out[hit, h, channel[e]] == (float("inf"), -float("inf"))[e])
+        out[hit, h, channel[e]] = clean[hit, h, channel[e]]
+        assert torch.equal(out[:, h], clean[:, h])
