@@ -131,7 +131,10 @@ class _CtypesCalls:
                 if kind == "G":
                     values.append(byref(arg))
                 elif kind in "CQ":
-                    values.append(byref(arg.desc()))
+                    desc = arg.desc()
+                    if isinstance(desc, PagedQ4) != (kind == "Q"):
+                        raise TypeError(f"{type(arg).__name__} is not the kind of cache that {name} takes")
+                    values.append(byref(desc))
                 elif kind == "S":
                     values.append(_stream(arg))
                 else:

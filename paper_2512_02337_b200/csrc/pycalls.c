@@ -115,18 +115,18 @@ static int pointer_of(PyObject *arg, uint64_t *out) {
     return data_ptr(arg, out);
 }
 
-/* The memory of a ctypes structure of at least `size` bytes; it lives as long as the structure does. */
-static int structure_of(PyObject *arg, size_t size, const void **out) {
+/* The memory of a ctypes structure of at least `size` bytes, or of exactly so many; it lives as long as the structure does. */
+static int structure_of(PyObject *arg, size_t size, int exactly, const void **out) {
     Py_buffer view;
     if (!PyObject_TypeCheck(arg, (PyTypeObject *)structure_type)) {
         PyErr_Format(PyExc_TypeError, "a ctypes structure was expected, not %.80s", Py_TYPE(arg)->tp_name);
         return -1;
     }
     if (PyObject_GetBuffer(arg, &view, PyBUF_SIMPLE)) return -1;
-    const int ok = view.len >= (Py_ssize_t)size;
+    const int ok = exactly ? view.len == (Py_ssize_t)size : view.len >= (Py_ssize_t)size;
     *out = view.buf;
     PyBuffer_Release(&view);
-    if (!ok) PyErr_Format(PyExc_TypeError, "%.80s is too small", Py_TYPE(arg)->tp_name);
+    if (!ok) PyErr_Format(PyExc_TypeError, exactly ? "%.80s is not what was expected" : "%.80s is too small", Py_TYPE(arg)->tp_name);
     return ok ? 0 : -1;
 }
 
@@ -135,7 +135,7 @@ static int cache_of(PyObject *cache, specpv_paged_kv *kv) {
     if ((PyObject *)Py_TYPE(cache) != cache_type) {
         const void *desc = NULL;
         PyObject *d = PyObject_CallMethodNoArgs(cache, s_desc);
-        const int bad = !d || structure_of(d, sizeof *kv, &desc);
+        const int bad = !d || structure_of(d, sizeof *kv, 0, &desc);
         if (!bad) *kv = *(const specpv_paged_kv *)desc;
         Py_XDECREF(d);
         return bad ? -1 : 0;
@@ -164,10 +164,11 @@ static int cache_of(PyObject *cache, specpv_paged_kv *kv) {
     return st;
 }
 
+/* (An ordinary cache's descriptor is larger: it is refused.) */
 static int q4_of(PyObject *cache, specpv_paged_q4 *kv) {
     const void *desc = NULL;
     PyObject *d = PyObject_CallMethodNoArgs(cache, s_desc);
-    const int bad = !d || structure_of(d, sizeof *kv, &desc);
+    const int bad = !d || structure_of(d, sizeof *kv, 1, &desc);
     if (!bad) *kv = *(const specpv_paged_q4 *)desc;
     Py_XDECREF(d);
     return bad ? -1 : 0;
@@ -175,7 +176,7 @@ static int q4_of(PyObject *cache, specpv_paged_q4 *kv) {
 
 static int config_of(PyObject *arg, uint64_t *out) {
     const void *cfg = NULL;
-    if (structure_of(arg, sizeof(specpv_config), &cfg)) return -1;
+    if (structure_of(arg, sizeof(specpv_config), 0, &cfg)) return -1;
     *out = (uint64_t)(uintptr_t)cfg;
     return 0;
 }
