@@ -426,7 +426,8 @@ specpv_status specpv_accumulate_attention(const specpv_config *cfg, int layer0, 
  * seq_lens[b] = keep_tokens.  Rows behind the new end keep what they held; shorter sequences are not touched.  idx (device,
  * [n_layers][batch][Hkv][keep_tokens]) receives the token that each place now holds (the first min(seq_lens[b], keep_tokens)).
  * keep_tokens < sink_tokens + local_tokens + 1 is SPECPV_ERR_BUDGET.  Pages must not be shared between sequences.  Block
- * summaries are not updated: specpv_update_block_summaries does that. */
+ * summaries are not updated: specpv_update_block_summaries does that.  After SPECPV_ERR_BAD_BLOCK_TABLE idx, acc and seq_lens are what they
+ * are without it, and a row that would come from or go to a page outside the pool has not moved: its place holds what it held. */
 specpv_status specpv_evict_tokens(const specpv_config *cfg, const specpv_paged_kv *kv, float *acc, int keep_tokens,
                                   int sink_tokens, int local_tokens, int32_t *idx, void *workspace, size_t workspace_bytes,
                                   void *stream);
