@@ -95,7 +95,12 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
                 const float natural = p.lse[((size_t)lb * p.M_max + row) * p.Hq + h * p.G + r % p.G];
                 if (natural != -INFINITY) {
                     lse = natural / p.scale;
-                    if (isfinite(lse)) rest = (float)(((double)lse - (double)natural / (double)p.scale) * (double)scale);
+                    if (isfinite(lse)) {
+                        rest = (float)(((double)lse - (double)natural / (double)p.scale) * (double)scale);
+                    } else {  // a scale too small for the quotient, or no number
+                        lse = 0.f;
+                        rest = -natural * 1.4426950408889634f;
+                    }
                     end = seq_len - n + a + 1;
                 }
             }

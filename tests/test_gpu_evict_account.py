@@ -44,3 +44,26 @@ def test_exact_products_and_a_large_log_sum_exp(dtype, d, bs, size):
                 tol[: len(w)] += w * (4 * 2.0 ** -24 * np.abs(x) + 2.0 ** -21)
         tol += 16 * 2.0 ** -24 * want  # a sum of 16
         assert np.all(np.abs(got[h, :n] - want) <= tol), (np.abs(got[h, :n] - want) / want).max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("scale", [1e-36, 1e-38, 1e-40, 1e-44])
+def test_scales_too_small_to_divide_by(dtype, scale):
+    """Scores of nothing: what counts is the log-sum-exp, which divided by such a scale is no float32."""
+    rng = np.random.default_rng(0)
+    Hq, Hkv, d, bs, n, M = 8, 2, 64, 16, 100, 3
+    cfg = config(1, Hq, Hkv, d, bs, dtype, softmax_scale=scale)
+    cache, _, _ = make_cache(1, Hkv, d, bs, [n], dtype, rng)
+    q = torch.from_numpy(rng.standard_normal((1, 1, M, Hq, d))).to(torch_dtype(dtype)).cuda()
+    lse = torch.from_numpy(np.log(n) + rng.standard_normal((1, 1, M, Hq))).float()
+    lse[0, 0, 0, 0], lse[0, 0, 1, 7] = -50.0, float("inf")
+    acc = torch.zeros(1, 1, Hkv, cache.block_table.shape[1] * bs, device="cuda")
+    ws = B.new_workspace(cfg, 1, 1, n, M)
+    B.specpv_accumulate_attention(cfg, 0, 1, q, lse.cuda(), M, None, torch.tensor([M], dtype=torch.int32, device="cuda"), M, cache, acc, ws)
+    assert B.specpv_poll_status(ws)[0] == 0
+    got, w = acc[0, 0].cpu().double().numpy(), np.exp(-lse[0, 0].double().numpy()).reshape(M, Hkv, -1).sum(-1)
+    for h in range(Hkv):
+        for t in range(n):
+            want = sum(w[i, h] for i in range(M) if t < n - M + i + 1)
+            # scores below 1e-34; the log-sum-exp times log2(e), in float32, its exponential, a sum of 12
+            assert abs(got[h, t] - want) <= want * (2 * 2.0 ** -24 * 50 * 1.45 + 2.0 ** -21 + 12 * 2.0 ** -24)
