@@ -391,7 +391,8 @@ specpv_status specpv_verify_full_q4(const specpv_config *cfg, int layer0, int n_
  * neither): the summaries of the blocks that received tokens, over the values that their keys stand for.  k_values / v_values (both
  * or neither; [n_layers_in_call][batch][A_max][Hkv][d] of cfg->dtype): what the appended rows stand for, so that a caller can append
  * the same numbers to another cache; rows >= n_accepted[b] are left as they were.  A row number outside [0, M_max) is
- * recorded as SPECPV_ERR_INVALID_ARG and its token left as its place was.  Pages that receive tokens belong to one sequence. */
+ * recorded as SPECPV_ERR_INVALID_ARG and its token left as its place was.  Pages that receive tokens belong to one sequence.  In
+ * the summaries NaN loses against numbers; a block of NaN keys alone has -infinity and +infinity, as in an ordinary cache. */
 specpv_status specpv_commit_accepted_q4(const specpv_config *cfg, int layer0, int n_layers, const void *k_new,
                                         const void *v_new, int M_max, const int32_t *accepted, const int32_t *n_accepted,
                                         int A_max, const specpv_paged_q4 *dst, void *kmax, void *kmin, void *k_values,

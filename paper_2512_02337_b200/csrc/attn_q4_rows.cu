@@ -59,8 +59,6 @@ struct RowsParams {
     const void* pool;
     const int32_t* block_table;
     const int32_t* seq_lens;
-    void* out;
-    float* lse;
     float* part_o;   // [lb][Hkv][slots][R_max][d]
     float* part_ml;  // [lb][Hkv][slots][R_max][2], the reference in units of log2, unrounded: the merge takes differences of them
     void* workspace;
@@ -682,7 +680,7 @@ bool attention_q4_rows_wanted(const AttnArgs& a) {
 specpv_status launch_attention_q4_rows(const AttnArgs& a, cudaStream_t stream) {
     RowsParams p{};
     p.q = a.q; p.k_new = a.k_new; p.v_new = a.v_new; p.tree_mask = a.tree_mask; p.q_lens = a.q_lens; p.pool = a.q4_pool;
-    p.block_table = a.block_table; p.seq_lens = a.seq_lens; p.out = a.out; p.lse = a.lse; p.workspace = a.workspace;
+    p.block_table = a.block_table; p.seq_lens = a.seq_lens; p.workspace = a.workspace;
     p.layer0 = a.layer0; p.batch = a.batch; p.M_max = a.M_max; p.mask_words = a.mask_words; p.Hq = a.g.Hq; p.Hkv = a.g.Hkv; p.G = a.g.G;
     p.bs = a.g.bs; p.bs_log2 = a.g.bs == 16 ? 4 : a.g.bs == 32 ? 5 : 6;
     p.max_blocks = a.max_blocks; p.n_pages = a.n_pages; p.n_layers = a.n_layers;
