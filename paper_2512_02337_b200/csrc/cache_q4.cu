@@ -17,7 +17,7 @@ namespace {
 // one pair.  A key's eight channels are a word as they are; a value's go to shared memory as such a word, and a thread then turns
 // the words of eight tokens over into words of eight channels, with those of tokens that the page held before.  The page's summary is
 // taken from the new keys in registers and the old ones' codes.  Bound by instructions (2048 rows x 8 heads x 16 layers of 128
-// channels: 105 us against 47 for its bytes, 300 instructions a token; with four channels a lane and values gathered byte by byte 165).
+// channels: 102 us against 47 for its bytes, 300 instructions a token; with four channels a lane and values gathered byte by byte 165).
 // grid = (pages touched, KV heads, layers x seqs).
 // ---------------------------------------------------------------------------------------------
 constexpr int kCommitThreads = 256;

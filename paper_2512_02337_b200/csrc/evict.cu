@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(32 * kAccWarps) accumulate_kernel(AccumulatePa
 // be read, because place j, as a source, belongs to a rank <= j.  For the same reason the next round's rows are requested before this
 // one's are written; where they are is known by then: one thread per row has asked for its index three rounds ahead and for the
 // table entries two ahead, so that no request waits for another.  Rows that stay are neither read nor written.  Bound by memory: every
-// moved row is read and written once (4096 of 4352 tokens, 8 heads x 32 layers: 222 us with the selection, 0.74 of the copy rate; with
+// moved row is read and written once (4096 of 4352 tokens, 8 heads x 32 layers: 224 us with the selection, 0.74 of the copy rate; with
 // each round's look-ups behind the round before 436).  grid = (cluster x 3 KV heads, layers x seqs).
 // ---------------------------------------------------------------------------------------------
 constexpr int kCloseThreads = 256;
@@ -412,8 +412,8 @@ __global__ void __launch_bounds__(kLensThreads) evict_lens_kernel(EvictParams p)
 
 template <typename T, int D>
 static specpv_status launch_accumulate_typed(AccumulateParams p, int n_layers, int max_seq_len, cudaStream_t stream) {
-    // Tiles per warp: the waves of CTAs, two on an SM, times what one takes, of which a start is about two and a half tiles (32 layers x 8
-    // heads x 4261 tokens, 20 rows: 73 us with 14 tiles per warp, 66 with the 17 chosen).
+    // Tiles per warp: the waves of CTAs, two on an SM (counted so for float32 with 128 channels as well, of which one fits), times what one takes,
+    // of which a start is about two and a half tiles (32 layers x 8 heads x 4261 tokens, 20 rows: 73 us with 14 tiles per warp, 66 with the 17 chosen).
     const long long tiles = (max_seq_len + kAccTokens - 1) / kAccTokens, heads = (long long)p.Hkv * n_layers * p.batch;
     int per_warp = 1;
     double best = 1e300;
