@@ -281,10 +281,12 @@ __global__ void __launch_bounds__(32 * RowsShape<D, NT>::kWarps, 1) attn_q4_rows
         }
         const float scale = p.scale_log2;
         auto any_coarse = [&](const float (&reference)[NT][2]) {
-            float largest = 0.f;
+            bool any = false;  // (of an infinite one nothing can be told apart: its row is NaN, and others' copy need not change)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) largest = fmaxf(largest, fmaxf(fabsf(reference[n][0]), fabsf(reference[n][1])));
-            return __any_sync(0xffffffffu, largest >= kCoarse) != 0;
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) any |= fabsf(reference[n][e]) >= kCoarse && fabsf(reference[n][e]) < INFINITY;
+            return __any_sync(0xffffffffu, any) != 0;
         };
         const uint32_t mask = p.q4_mask, ones = p.q4_ones;
         // (Copies of the code: where a branch chose between opened codes and the step's own rows, every fragment was moved once more.  A branch

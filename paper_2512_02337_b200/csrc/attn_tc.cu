@@ -771,7 +771,7 @@ __device__ __forceinline__ void softmax(const TcParams& p, const Job& c, Barrier
             }
             float m_use = m_run == -INFINITY ? 0.f : m_run;
             if constexpr (kQ4) {
-                coarse = __any_sync(0xffffffffu, fabsf(m_use) >= kCoarse);
+                coarse = __any_sync(0xffffffffu, fabsf(m_use) >= kCoarse && fabsf(m_use) < INFINITY);  // (an infinite one's row is NaN)
                 if (coarse) {  // exp_row's product is then off by 2^-24 of a difference, not of a score
                     const float back = 1.f / p.scale_log2;  // (finite: a scale below 2^-104 makes no score of 2^24)
 #pragma unroll

@@ -173,3 +173,40 @@ def test_infinite_values_of_hardly_any_weight(dtype, d, M, n):
         assert torch.all(out[hit, h, channel[e]] == (float("inf"), -float("inf"))[e])
         out[hit, h, channel[e]] = clean[hit, h, channel[e]]
         assert torch.equal(out[:, h], clean[:, h])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("M,n", [(4, 150), (4, 2000), (12, 150), (40, 700)])
+def test_infinite_keys_reach_only_the_rows_that_see_them(dtype, d, M, n):
+    """A score of -infinity is a token that is not there, one of +infinity no number; other rows keep every bit."""
+    rng = np.random.default_rng(M + d)
+    Hq, Hkv = 8, 2
+    q4 = Q.Q4(1, Hkv, d, 64, [n], seed=2)
+    q, _ = rows(rng, (1, 1, M, Hq, d), dtype)
+    q[..., 5] = q[..., 5].abs().clamp(min=0.5) * torch.from_numpy(rng.choice([-1.0, 1.0], (1, 1, M, Hq))).to(q.dtype).cuda()
+    k, _ = rows(rng, (1, 1, M, Hkv, d), dtype)
+    v, _ = rows(rng, (1, 1, M, Hkv, d), dtype)
+    seen = rng.random((M, M)) < 0.5
+    seen[range(M), range(M)] = True
+
+    def words(s):
+        w = np.zeros((1, M, (M + 63) // 64), np.uint64)
+        for j in range(M):
+            w[0, :, j // 64] |= s[:, j].astype(np.uint64) << np.uint64(j % 64)
+        return torch.from_numpy(w.view(np.int64)).cuda()
+
+    clean, clean_lse = verify(dtype, Hq, Hkv, d, q4, q, k, v, words(seen), M)
+    without = seen.copy()
+    without[:, 2] = False
+    less, less_lse = verify(dtype, Hq, Hkv, d, q4, q, k, v, words(without), M)
+    k[0, 0, 2, :, 5] = float("inf")
+    out, lse = verify(dtype, Hq, Hkv, d, q4, q, k, v, words(seen), M)
+    for j in range(M):
+        for h in range(Hq):
+            if not seen[j, 2]:
+                assert torch.equal(out[j, h], clean[j, h]) and lse[j, h] == clean_lse[j, h]
+            elif q[0, 0, j, h, 5] < 0:
+                assert torch.equal(out[j, h], less[j, h]) and lse[j, h] == less_lse[j, h]
+            else:
+                assert out[j, h].isnan().all() and lse[j, h].isnan()
